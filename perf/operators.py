@@ -192,7 +192,7 @@ def prepare(case, seed):
             s["logprob"] = torch.empty(c["rows"], device="cuda")
         else:
             s["layer"] = snn.SequenceLayer(c["B"], c.get("T", 1), c["C"], state=c.get("N", 1), groups=c.get("G", 1),
-                                           taps=c.get("K", 1), train="dy" in s)
+                                           taps=c.get("K", 1), train="dy" in s, recompute=c["op"] == "scan_packed")
     return s
 
 
@@ -405,7 +405,7 @@ def _plain(s):
         return _plain_scan(s, s["u"].float(), s["delta"].float(), s["z"].float() if s["z"] is not None else None,
                            _scan_outputs(s["case"], True, s["case"]["train"]))
     if op == "scan_packed":
-        # the forward pass reads the activations, and keeps its states; the backward pass takes u, delta and z from 8 bits
+        # the forward pass reads the activations; the backward pass takes u, delta and z, and the states that they give, from 8 bits
         out = _plain_scan(s, s["u"].float(), s["delta"].float(), s["z"].float(), _scan_outputs(s["case"], True, False))
         return dict(out, **_plain_scan(s, _packed(s["u"]), _packed(s["delta"]), _packed(s["z"]),
                                        _scan_outputs(s["case"], False, True)))
@@ -458,7 +458,8 @@ def _own(s):
         L.scan_step(s["u"], s["delta"], s["A"], s["Bm"], s["Cm"], s["h"], h, y, D=s["D"], z=s["z"], delta_bias=s["delta_bias"])
         return {"y": y, "h": h}
     u, delta, z = s["u"], s["delta"], s["z"]
-    saved = torch.empty(L.saved_shape, device="cuda") if "dy" in s else None
+    # the states of packed activations are computed again with them
+    saved = torch.empty(L.saved_shape, device="cuda") if "dy" in s and op != "scan_packed" else None
     out = {"y": torch.empty_like(u), "h": torch.empty_like(s["h0"])}
     L.scan_forward(u, delta, s["A"], s["Bm"], s["Cm"], out["y"], D=s["D"], z=z, delta_bias=s["delta_bias"], h0=s["h0"],
                    hT=out["h"], saved=saved, lengths=s["lengths"])
@@ -477,7 +478,7 @@ def _own(s):
         out["dz"] = torch.empty_like(s["dy"])
     L.scan_backward(u, delta, s["A"], s["Bm"], s["Cm"], s["dy"], saved, out["du"], out["ddelta"], out["dA"], out["dB"],
                     out["dC"], D=s["D"], z=z, delta_bias=s["delta_bias"], dD=out["dD"], dz=out.get("dz"),
-                    ddelta_bias=out["ddelta_bias"], dh0=out["dh0"], lengths=s["lengths"])
+                    ddelta_bias=out["ddelta_bias"], h0=s["h0"], dh0=out["dh0"], lengths=s["lengths"])
     return out
 
 
