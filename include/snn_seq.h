@@ -1,0 +1,255 @@
+/*
+ * snn_seq.h -- C ABI of libsnn's sequence operators: operators over dense
+ * [batch][T][n] sequences, for the trials that the spiking networks of snn.h
+ * run on, on AMD Instinct MI355X (gfx950).
+ *
+ *   bin     spike lists (snn.h's input CSR or its records) -> spike counts per
+ *           bin of steps
+ *   conv    short causal convolution of each channel with its own taps, SiLU
+ *   scan    selective state-space scan: a leaky integrator of `state` states
+ *           per channel whose decay and input depend on the sequence
+ *   pack    activations in 8 bits with a scale per 128 channels, and back; the
+ *           backward passes of conv and scan read the packed form
+ *   sample  a class drawn from a row of scores by given random numbers, after
+ *           temperature, top-k, top-p and min-p (its own handle, snn_sampler)
+ *
+ * conv and scan have a forward pass, a backward pass and a form for a single
+ * step of every sample.  Everything is computed in fp32 whatever the tensors'
+ * type, and rounded once to the type of an output; sums are taken in a fixed
+ * order, so results are the same from call to call.
+ *
+ * Memory and streams.  Every pointer is device memory of the handle's device
+ * (the one current in create), owned by the caller, unless marked (host).
+ * Outputs are fully overwritten and must not overlap inputs, except where
+ * stated.  A handle owns its scratch, allocated in create; no other call
+ * allocates, waits for the device or reads back: a call checks its arguments,
+ * enqueues its kernels on the handle's stream and returns, so it can be
+ * captured into a graph.  Calls on one handle share its scratch: graphs
+ * captured from one handle must not run at the same time as each other or as
+ * its calls on another stream.  Distinct handles are independent.  A handle
+ * is not thread-safe.
+ *
+ * Lengths.  `lengths` [batch] (or NULL: T each) gives the valid steps of each
+ * sample, clamped to [0, T]: what lies behind them is not read (it may hold
+ * anything, NaN included), is written as zero in every [batch][T][n] output,
+ * and changes neither states nor gradients.  A sample of length 0 ends in the
+ * state it started from.
+ *
+ * Errors: SNN_EINVAL (bad sizes, types, strides or NULL pointers; nothing is
+ * enqueued), SNN_ENOMEM, SNN_EDEVICE; snn_seq_last_error has the message.
+ */
+#ifndef SNN_SEQ_H
+#define SNN_SEQ_H
+
+#include "snn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { SNN_F32 = 0, SNN_BF16 = 1, SNN_F16 = 2, SNN_E4M3 = 3 };   /* element types */
+
+#define SNN_SEQ_BLOCK 128        /* channels that share a scale in the packed form */
+#define SNN_SEQ_SEGMENT 16       /* steps between the states that scan_forward saves */
+#define SNN_SEQ_MAX_CHANNELS 65536
+#define SNN_SEQ_MAX_STATE 64
+#define SNN_SEQ_MAX_TAPS 8
+
+/* A [batch][T][n] sequence: element (b, t, c) at data[b * sample + t * row + c]
+ * (strides in elements, row >= n, sample >= 0).  SNN_E4M3 is the packed form:
+ * contiguous bytes, value = scale[(b * T + t) * ceil(n / 128) + c / 128] *
+ * e4m3(byte); scale is unused otherwise. */
+typedef struct {
+    void* data;
+    float* scale;
+    int64_t row, sample;
+    int32_t dtype;
+} snn_tensor;
+
+typedef struct snn_seq snn_seq;
+
+/*
+ * batch, T:      samples and steps of every call (step calls: one step)
+ * channels:      channels of conv and scan
+ * state, groups: states per channel, and groups of channels / groups
+ *                neighbouring channels that share one B and C (groups divides
+ *                channels)
+ * taps:          taps of conv
+ * flags:         SNN_SEQ_TRAIN: the backward passes will be called;
+ *                SNN_SEQ_RECOMPUTE (with SNN_SEQ_TRAIN): scan_backward will be
+ *                called without saved states (scratch of snn_seq_saved floats)
+ * hip_stream:    hipStream_t to enqueue on (NULL: default stream)
+ */
+#define SNN_SEQ_TRAIN 1
+#define SNN_SEQ_RECOMPUTE 2
+typedef struct {
+    int32_t batch, T, channels, state, groups, taps, flags;
+    void* hip_stream;
+} snn_seq_opts;
+
+int snn_seq_create(const snn_seq_opts* opts, snn_seq** out);
+const char* snn_seq_last_error(const snn_seq* seq);   /* as snn_last_error */
+void snn_seq_destroy(snn_seq* seq);                   /* waits for its stream */
+
+/*
+ * Spike counts: dst[b][r][c] = spikes of neuron c of sample b in steps
+ * [r factor, (r + 1) factor), r < ceil(T / factor), 1 <= factor <= T; dst has
+ * ceil(T / factor) rows of n <= SNN_MAX_INPUT channels in any type but
+ * SNN_E4M3 (counts past 2048 round in SNN_F16, past 256 in SNN_BF16).
+ * bin_spikes reads snn.h's input lists, bin_records one layer's records of
+ * [batch][capacity] (stored records only: min(count, capacity)).  A sample's
+ * events are in order of their step; an event outside [0, T) x [0, n) is left
+ * out.
+ */
+int snn_seq_bin_spikes(snn_seq* seq, const snn_spikes_in* in, int32_t n, int32_t factor,
+                       const snn_tensor* dst);
+int snn_seq_bin_records(snn_seq* seq, const snn_spikes_out* rec, int32_t capacity, int32_t n,
+                        int32_t factor, const snn_tensor* dst);
+
+/*
+ * Packed activations: with the largest finite |x| of a (step, block of 128
+ * channels), the scale is the least power of two 2^k >= 2^-126 with
+ * |x| <= 448 2^k (1 for a block of zeros), and the byte the e4m3 value nearest
+ * to x / scale (ties to even); infinities and NaN become NaN.  A power of two
+ * makes the division exact, so the byte is the value's own rounding: its
+ * relative error is at most 2^-4 down to 2^-6 of the scale.
+ * x: [batch][T][n]; q: SNN_E4M3 with data [batch][T][n] bytes.
+ */
+int snn_seq_pack(snn_seq* seq, int32_t n, const snn_tensor* x, const snn_tensor* q);
+int snn_seq_unpack(snn_seq* seq, int32_t n, const snn_tensor* q, const snn_tensor* x);
+
+/*
+ * Causal convolution:
+ *   pre[t, c] = bias[c] + sum_{k < taps} w[c][k] x[t - (taps - 1) + k, c]
+ *   y = pre sigmoid(pre) (silu != 0) or pre
+ * x before the first step is `state` [batch][taps - 1][channels] of x's type,
+ * oldest first, or zero (NULL).  state_out gets the last taps - 1 inputs of
+ * each sample (of state and x together), and must not be state itself.
+ */
+typedef struct {
+    snn_tensor x, y;
+    const float* w;          /* [channels][taps] */
+    const float* bias;       /* [channels] or NULL */
+    const int32_t* lengths;  /* [batch] or NULL */
+    const void* state;       /* or NULL */
+    void* state_out;         /* or NULL */
+    int32_t silu;
+} snn_seq_conv;
+int snn_seq_conv_forward(snn_seq* seq, const snn_seq_conv* a);
+
+/* dx, dw, dbias (NULL: not wanted) and dstate [batch][taps - 1][channels] (or
+ * NULL) from dy and dstate_out (the gradient of state_out, or NULL: zero), of
+ * the forward's inputs; x may be packed (its values are then what the
+ * formulas take).  dy, dx, state, dstate_out and dstate have one type, x's
+ * unless x is packed. */
+typedef struct {
+    snn_tensor x, dy, dx;
+    const float* w;
+    const float* bias;
+    float* dw;
+    float* dbias;
+    const int32_t* lengths;
+    const void* state;
+    const void* dstate_out;
+    void* dstate;
+    int32_t silu;
+} snn_seq_conv_grad;
+int snn_seq_conv_backward(snn_seq* seq, const snn_seq_conv_grad* a);
+
+/* One step: x, y [batch][channels] (their strides: sample; row is not used),
+ * state_out may be state. */
+int snn_seq_conv_step(snn_seq* seq, const snn_seq_conv* a);
+
+/*
+ * Selective scan.  With delta' = softplus(delta + delta_bias) (softplus != 0)
+ * or delta + delta_bias, per channel c of group g and state n:
+ *   h[t] = exp(delta'[t] A[c][n]) h[t - 1] + delta'[t] u[t] B[t][g][n]
+ *   y[t] = (sum_n C[t][g][n] h[t] + D[c] u[t]) silu(z[t])
+ * B, C: sequences of groups * state channels.  z.data NULL: no gate (factor
+ * 1); D, delta_bias NULL: zero; h0 NULL: zero.  hT [batch][channels][state]
+ * gets each sample's last state.  saved, for the backward pass: snn_seq_saved
+ * floats, written here (NULL: none).  u, delta, B, C, z and y have one type.
+ */
+typedef struct {
+    snn_tensor u, delta, B, C, z, y;
+    const float* A;          /* [channels][state] */
+    const float* D;          /* [channels] or NULL */
+    const float* delta_bias; /* [channels] or NULL */
+    const float* h0;         /* [batch][channels][state] or NULL */
+    float* hT;               /* [batch][channels][state] or NULL */
+    float* saved;            /* or NULL */
+    const int32_t* lengths;
+    int32_t softplus;
+} snn_seq_scan;
+int snn_seq_scan_forward(snn_seq* seq, const snn_seq_scan* a);
+int snn_seq_saved(const snn_seq* seq, int64_t* floats);   /* floats of `saved` (16-byte aligned) */
+
+/* Gradients of the forward's inputs from dy and dhT (the gradient of hT, or
+ * NULL: zero).  Of u, delta and z each may be packed; the formulas then take
+ * the packed values.  saved: as the forward wrote it, or NULL: the states are
+ * computed again from u, delta, B and h0 (SNN_SEQ_RECOMPUTE), which is what
+ * belongs to packed u and delta: the states saved from the unpacked ones are
+ * not those of the packed values.  h0 is read only then.  dD, ddelta_bias and
+ * dh0 may be NULL (not wanted); dz.data is NULL exactly where z.data is. */
+typedef struct {
+    snn_tensor u, delta, B, C, z, dy, du, ddelta, dB, dC, dz;
+    const float* A;
+    const float* D;
+    const float* delta_bias;
+    const float* h0;
+    const float* dhT;
+    const float* saved;
+    float* dA;               /* [channels][state] */
+    float* dD;
+    float* ddelta_bias;
+    float* dh0;
+    const int32_t* lengths;
+    int32_t softplus;
+} snn_seq_scan_grad;
+int snn_seq_scan_backward(snn_seq* seq, const snn_seq_scan_grad* a);
+
+/* One step: sequences [batch][n] (their strides: sample; row is not used);
+ * h0 and hT are the states before and after, and may be the same. */
+int snn_seq_scan_step(snn_seq* seq, const snn_seq_scan* a);
+
+/*
+ * Sampling.  Per row, with m the row's largest score (NaN counts as -inf):
+ * weight_i = exp((score_i - m) / temperature); scores in falling order, equal
+ * ones by index; kept are the first top_k of them (top_k <= 0: all), those
+ * before which less than top_p of the row's total weight lies (top_p >= 1:
+ * all; top_p <= 0: the first), and of these the ones of at least min_p
+ * (min_p <= 0: all; above 1: as 1).  token is the first index
+ * (in index order) at which the running sum of the kept weights is above u
+ * times their total, logprob the log of its share of that total.  temperature <= 0: the first
+ * of the largest scores, logprob 0.  A row where +inf occurs is drawn from
+ * its +inf alone, alike; a row of nothing but -inf and NaN gives token -1,
+ * logprob -inf.  The sums are exact: a weight is rounded once, from fp64 to a
+ * whole number of 2^-(62 - ceil(log2 n)).  u, temperature, top_p, min_p [rows]
+ * fp32, top_k [rows]; each but u may be NULL (1, all, 1, 0).  NaN in them
+ * counts as their default, u outside [0, 1) as the nearest number inside.
+ */
+typedef struct snn_sampler snn_sampler;
+typedef struct {
+    const void* scores;      /* row r at scores + r * row (elements, row >= n) */
+    int64_t row;
+    int32_t dtype;           /* SNN_F32, SNN_BF16 or SNN_F16 */
+    int32_t rows, n;         /* at most the handle's */
+    const float* u;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    int32_t* token;          /* [rows] */
+    float* logprob;          /* [rows] or NULL */
+} snn_sample_args;
+#define SNN_SAMPLE_MAX_N (1 << 24)
+int snn_sampler_create(int32_t rows, int32_t n, void* hip_stream, snn_sampler** out);
+int snn_sampler_sample(snn_sampler* s, const snn_sample_args* a);
+const char* snn_sampler_last_error(const snn_sampler* s);
+void snn_sampler_destroy(snn_sampler* s);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* SNN_SEQ_H */

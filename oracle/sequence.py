@@ -1,0 +1,208 @@
+"""The sequence operators (include/snn_seq.h) in fp64, step by step: plain
+numpy, for the checks of the library.
+
+``absolute`` replaces every term of the sums by its absolute value: the size
+that the rounding errors of an output are relative to.
+"""
+import numpy as np
+
+
+def _lengths(lengths, B, T):
+    return np.full(B, T, np.int64) if lengths is None else np.clip(np.asarray(lengths, np.int64), 0, T)
+
+
+def sigmoid(x):
+    return 1.0 / (1.0 + np.exp(-x))
+
+
+def silu(x):
+    return x * sigmoid(x)
+
+
+def dsilu(x):
+    p = sigmoid(x)
+    return p * (1.0 + x * (1.0 - p))
+
+
+def bin_spikes(lists, T, n, factor):
+    """lists: (step, neuron) arrays per sample -> counts [B][ceil(T/factor)][n]."""
+    out = np.zeros((len(lists), -(-T // factor), n))
+    for b, (step, neuron) in enumerate(lists):
+        for s, c in zip(step, neuron):
+            if 0 <= s < T and 0 <= c < n:
+                out[b, s // factor, c] += 1
+    return out
+
+
+def conv(x, w, bias=None, lengths=None, state=None, act=True, dy=None, dstate_out=None, absolute=False):
+    """(y, state_out), and with dy also the gradients, as a dict."""
+    B, T, C = x.shape
+    K = w.shape[1]
+    L = _lengths(lengths, B, T)
+    bias = np.zeros(C) if bias is None else bias
+    f, df = (silu, dsilu) if act else (lambda v: v, np.ones_like)
+    mag = np.abs if absolute else (lambda v: v)
+    out = {"y": np.zeros((B, T, C)), "state_out": np.zeros((B, K - 1, C))}
+    if dy is not None:
+        out.update(dx=np.zeros((B, T, C)), dw=np.zeros((C, K)), dbias=np.zeros(C), dstate=np.zeros((B, K - 1, C)))
+    for b in range(B):
+        # the state and the sample's inputs as one line; line[t + K - 1] is x[t]
+        line = np.concatenate([np.zeros((K - 1, C)) if state is None else state[b], x[b, :L[b]]])
+        dline = np.zeros_like(line)
+        out["state_out"][b] = line[len(line) - (K - 1):]
+        if dstate_out is not None:
+            dline[len(line) - (K - 1):] += mag(dstate_out[b])
+        for t in range(L[b]):
+            win = line[t:t + K]                               # [K, C]
+            pre = bias + (w.T * win).sum(0)
+            size = np.abs(bias) + np.abs(w.T * win).sum(0)
+            out["y"][b, t] = size if absolute else f(pre)     # |act'| is at most 1.1
+            if dy is None:
+                continue
+            g = mag(dy[b, t]) * (1.1 * (1.0 + size) if absolute else df(pre))
+            out["dw"] += (g * mag(win)).T
+            out["dbias"] += g
+            dline[t:t + K] += mag(w.T) * g
+        if dy is not None:
+            out["dstate"][b] = dline[:K - 1]
+            out["dx"][b, :L[b]] = dline[K - 1:]
+    return out
+
+
+def softplus(x):
+    return np.logaddexp(0.0, x)
+
+
+def scan(u, delta, A, Bm, Cm, D=None, z=None, delta_bias=None, h0=None, lengths=None, plus=True, dy=None, dhT=None,
+         absolute=False):
+    """y and hT, and with dy every gradient, as a dict.  Bm, Cm: [B][T][G][N]."""
+    B, T, C = u.shape
+    N, G = A.shape[1], Bm.shape[2]
+    L = _lengths(lengths, B, T)
+    group = np.arange(C) // (C // G)
+    D = np.zeros(C) if D is None else D
+    bias = np.zeros(C) if delta_bias is None else delta_bias
+    mag = np.abs if absolute else (lambda v: v)
+    out = {"y": np.zeros((B, T, C)), "hT": np.zeros((B, C, N))}
+    if dy is not None:
+        for k in ("du", "ddelta", "dz"):
+            out[k] = np.zeros((B, T, C))
+        out.update(dB=np.zeros((B, T, G, N)), dC=np.zeros((B, T, G, N)), dA=np.zeros((C, N)), dD=np.zeros(C),
+                   ddelta_bias=np.zeros(C), dh0=np.zeros((B, C, N)))
+    for b in range(B):
+        h = np.zeros((C, N)) if h0 is None else mag(h0[b])
+        hs, y0s = [], []
+        for t in range(L[b]):
+            hs.append(h)
+            raw = delta[b, t] + bias
+            d = softplus(raw) if plus else raw
+            a = np.exp(d[:, None] * A)
+            h = a * h + mag((d * u[b, t])[:, None] * Bm[b, t][group])
+            y0s.append((mag(Cm[b, t][group]) * h).sum(1) + mag(D * u[b, t]))
+            out["y"][b, t] = y0s[-1] * (mag(silu(z[b, t])) if z is not None else 1.0)
+        out["hT"][b] = h
+        if dy is None:
+            continue
+        g = np.zeros((C, N)) if dhT is None else mag(dhT[b])
+        for t in reversed(range(L[b])):
+            raw = delta[b, t] + bias
+            d, sig = (softplus(raw), sigmoid(raw)) if plus else (raw, np.ones(C))
+            a = np.exp(d[:, None] * A)
+            Bt, Ct, ut = Bm[b, t][group], Cm[b, t][group], u[b, t]
+            q = mag(dy[b, t])
+            if z is not None:
+                # silu' = p + z p (1 - p): its terms cancel near z = -1.28
+                slope = sigmoid(z[b, t]) * (1 + mag(z[b, t]) * sigmoid(-z[b, t]))
+                out["dz"][b, t] = q * y0s[t] * slope
+                q = q * mag(silu(z[b, t]))
+            ht = a * hs[t] + mag((d * ut)[:, None] * Bt)
+            g = g + mag(Ct) * q[:, None]
+            np.add.at(out["dC"][b, t], group, q[:, None] * ht)
+            np.add.at(out["dB"][b, t], group, g * mag(d * ut)[:, None])
+            gb = (g * mag(Bt)).sum(1)
+            ga = g * a * hs[t]
+            out["dA"] += ga * mag(d)[:, None]
+            out["dD"] += q * mag(ut)
+            out["du"][b, t] = mag(D) * q + mag(d) * gb
+            out["ddelta"][b, t] = ((ga * mag(A)).sum(1) + mag(ut) * gb) * sig
+            g = a * g
+        out["dh0"][b] = g
+    if dy is not None:
+        out["ddelta_bias"] = out["ddelta"].sum((0, 1))
+    return out
+
+
+def e4m3_values():
+    """The 127 finite non-negative e4m3 values, by code."""
+    code = np.arange(127)
+    m, e = code % 8, code // 8
+    return np.where(e == 0, m * 2.0 ** -9, (1 + m / 8) * 2.0 ** (e - 7.0))
+
+
+def pack(x, block=128):
+    """(bytes, scales) of x [B][T][n]."""
+    grid = e4m3_values()
+    B, T, n = x.shape
+    q = np.zeros((B, T, n), np.uint8)
+    scale = np.ones((B, T, -(-n // block)))
+    for b in range(B):
+        for t in range(T):
+            for k in range(scale.shape[2]):
+                v = x[b, t, k * block:(k + 1) * block].astype(np.float64)
+                fine = np.isfinite(v)
+                top = np.abs(v[fine]).max() if fine.any() else 0.0
+                e = 0
+                if top > 0:
+                    e = max(-126, int(np.ceil(np.log2(top / 448.0))))
+                    while 448.0 * 2.0 ** e < top:
+                        e += 1
+                    while e > -126 and 448.0 * 2.0 ** (e - 1) >= top:
+                        e -= 1
+                scale[b, t, k] = 2.0 ** e
+                r = np.abs(np.where(fine, v, 0.0)) / 2.0 ** e
+                hi = np.clip(np.searchsorted(grid, r), 1, 126)
+                lo = hi - 1
+                up = (r - grid[lo] > grid[hi] - r) | ((r - grid[lo] == grid[hi] - r) & (hi % 2 == 0))
+                code = np.where(up, hi, lo) + 128 * np.signbit(v)
+                q[b, t, k * block:(k + 1) * block] = np.where(fine, code, 0x7F)
+    return q, scale
+
+
+def unpack(q, scale, block=128):
+    grid = np.concatenate([e4m3_values(), [np.nan]])
+    v = np.where(q >= 128, -1.0, 1.0) * grid[q & 0x7F]
+    return v * np.repeat(scale, block, axis=2)[:, :, :q.shape[2]]
+
+
+def sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, logprob, kept indices) of one row of scores."""
+    z = np.where(np.isnan(z), -np.inf, z.astype(np.float64))
+    top = z.max()
+    if np.isneginf(top):
+        return -1, -np.inf, []
+    if temperature <= 0:
+        return int(np.argmax(z)), 0.0, [int(np.argmax(z))]
+    x = np.zeros_like(z)
+    if np.isposinf(top):
+        x = np.where(z == top, 0.0, np.inf)
+    else:
+        x = (top - z) / temperature
+    w = np.exp(-x)
+    order = np.argsort(-z, kind="stable")
+    total = w.sum()
+    kept, before = [], 0.0
+    for rank, i in enumerate(order):
+        if top_k > 0 and rank >= top_k:
+            break
+        if rank and top_p < 1.0 and not before < top_p * total:
+            break
+        if np.isneginf(z[i]) or (rank and w[i] < min(min_p, 1.0)):
+            break
+        kept.append(int(i))
+        before += w[i]
+    kept.sort()
+    run = np.cumsum(w[kept])
+    u = min(max(u, 0.0), 1.0 - 2.0 ** -24)
+    j = int(np.searchsorted(run, u * run[-1], side="right"))
+    j = min(j, len(kept) - 1)
+    return kept[j], float(np.log(w[kept[j]] / run[-1])), kept

@@ -11,10 +11,13 @@ from .binding import (SNNError, SNNOverflow, Network, lib_path, load_library, SN
                       SNN_LI, SNN_LOSS_CE_SUM, SNN_LOSS_CE_MAX, SNN_LOSS_DMSE, SNN_FLAG_HBM_RINGS,
                       SNN_FLAG_TIMING, SNN_FLAG_SEPARATE_READOUT, SNN_FLAG_CLUSTER, SNN_OPT_SGD, SNN_OPT_ADAM, SNN_OK, SNN_EINVAL, SNN_ENOMEM,
                       SNN_ESTATE, SNN_EOVERFLOW, SNN_EDEVICE, SNN_NOALLOC_SCRATCH_BYTES)
+from .sequence import (Packed, Sampler, SequenceLayer, SNN_F32, SNN_BF16, SNN_F16, SNN_E4M3, SNN_SEQ_BLOCK, SNN_SEQ_SEGMENT,
+                       SNN_SEQ_TRAIN, SNN_SEQ_RECOMPUTE, SNN_SAMPLE_MAX_N, SNN_SEQ_MAX_CHANNELS, SNN_SEQ_MAX_STATE, SNN_SEQ_MAX_TAPS)
 from . import schedules
 
 __all__ = ["SNNError", "SNNOverflow", "Network", "lib_path", "load_library", "SNN_INPUT", "SNN_LIF",
            "SNN_LI", "SNN_LOSS_CE_SUM", "SNN_LOSS_CE_MAX", "SNN_LOSS_DMSE", "SNN_FLAG_HBM_RINGS",
            "SNN_FLAG_TIMING", "SNN_FLAG_SEPARATE_READOUT", "SNN_FLAG_CLUSTER", "SNN_OPT_SGD", "SNN_OPT_ADAM", "SNN_OK", "SNN_EINVAL", "SNN_ENOMEM",
            "SNN_ESTATE", "SNN_EOVERFLOW", "SNN_EDEVICE", "SNN_NOALLOC_SCRATCH_BYTES",
-           "schedules"]
+           "Packed", "Sampler", "SequenceLayer", "SNN_F32", "SNN_BF16", "SNN_F16", "SNN_E4M3", "SNN_SEQ_BLOCK", "SNN_SEQ_SEGMENT",
+           "SNN_SEQ_TRAIN", "SNN_SEQ_RECOMPUTE", "SNN_SAMPLE_MAX_N", "SNN_SEQ_MAX_CHANNELS", "SNN_SEQ_MAX_STATE", "SNN_SEQ_MAX_TAPS", "schedules"]

@@ -294,6 +294,21 @@ class Network:
     def optimizer_reset(self):
         return self._check(self._lib.snn_optimizer_reset(self._h))
 
+    def sample(self, z, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None):
+        """A class for each sample drawn from its readout values z [B][C]
+        (forward's, cross-entropy losses) by the random numbers u [B]; the
+        other arguments as Sampler.sample, which this calls on a sampler of
+        the handle's stream."""
+        from .sequence import Sampler
+        if self.layers[-1][1] == SNN_LIF:
+            raise ValueError("z holds first spike times: they are not scores to draw from")
+        C_ = self.layers[-1][0]
+        if z.numel() != self.batch * C_:
+            raise ValueError("z must hold B x C elements")
+        if getattr(self, "_sampler", None) is None:
+            self._sampler = Sampler(self.batch, C_, stream=self.stream)
+        self._sampler.sample(z.view(self.batch, C_), u, token, temperature, top_k, top_p, min_p, logprob)
+
     def state(self, layer: int, V, I):
         import torch
         rc = self._lib.snn_get_state(self._h, int(layer), _ptr(V, torch.float32, "V"),

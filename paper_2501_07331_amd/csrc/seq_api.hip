@@ -1,0 +1,582 @@
+// Host side of the sequence operators: checks of arguments, scratch and the
+// division of the work.  See include/snn_seq.h for the contract.
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "seq_internal.h"
+#include "seq_sample.h"
+
+namespace {
+
+// The handle's device is current while a call lasts.
+struct OnDevice {
+    int before = -1;
+    hipError_t err;
+    explicit OnDevice(int dev) {
+        err = hipGetDevice(&before);
+        if (err == hipSuccess && before != dev) err = hipSetDevice(dev);
+        else before = -1;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+// Parts of the time axis: a single one where there are workgroups for the
+// chip's 256 CUs without a division, since the parts' starts cost a second
+// pass over the inputs; otherwise as many as fill it twice, of at least 64
+// steps.  len: steps a part, whole tiles.
+void time_parts(int T, long long workgroups, int* parts, int* len) {
+    const long long want = workgroups >= 256 ? 1 : (512 + workgroups - 1) / workgroups;
+    const int tiles = (T + kScanTile - 1) / kScanTile;
+    const int per = std::max(2, (int)((tiles + want - 1) / want));
+    *len = std::min(per, tiles) * kScanTile;
+    *parts = (T + *len - 1) / *len;
+}
+
+}  // namespace
+
+struct snn_seq {
+    snn_seq_opts o;
+    hipStream_t stream;
+    int device;
+    int np, gblocks, segs, parts, part_len;
+    char* mem;                         // one allocation
+    float *carry, *dsum;               // states between the parts of the time axis
+    float *bcpart, *apart, *dpart;     // shares of the scan's gradients
+    float* cpart;                      // shares of the convolution's; the scan's memory
+    float* states;                     // the scan's states, computed again
+    char err[512];
+};
+
+namespace {
+thread_local char g_seq_err[512];
+
+int fail(snn_seq* s, int code, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(s->err, sizeof s->err, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+int create_fail(int code, const char* what, const char* why) {
+    snprintf(g_seq_err, sizeof g_seq_err, "%s%s%s", what, why ? ": " : "", why ? why : "");
+    return code;
+}
+
+#define SEQ_TRY(s, expr)                                                                         \
+    do {                                                                                         \
+        const hipError_t e_ = (expr);                                                            \
+        if (e_ != hipSuccess) return fail((s), SNN_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
+    } while (0)
+
+#define SEQ_ENTER(s)                       \
+    if (!(s)) return SNN_EINVAL;           \
+    (s)->err[0] = 0;                       \
+    OnDevice on_device_((s)->device);      \
+    SEQ_TRY(s, on_device_.err)
+
+// A sequence argument of n channels and T steps.  type < 0: any dense type;
+// otherwise that type.  packed: SNN_E4M3 will do too.
+int seq_arg(snn_seq* s, const snn_tensor& t, const char* name, int n, int T, int type, bool packed, SeqT* out) {
+    if (!t.data) return fail(s, SNN_EINVAL, "%s: NULL data", name);
+    memset(out, 0, sizeof *out);
+    out->p = static_cast<char*>(t.data);
+    if (t.dtype == SNN_E4M3) {
+        if (!packed) return fail(s, SNN_EINVAL, "%s: the packed form is not taken here", name);
+        if (!t.scale) return fail(s, SNN_EINVAL, "%s: NULL scale of a packed sequence", name);
+        out->scale = t.scale;
+        out->packed = 1;
+        out->blocks = (n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK;
+        out->row = n;
+        out->sample = (long long)n * T;
+        return SNN_OK;
+    }
+    if (t.dtype != SNN_F32 && t.dtype != SNN_BF16 && t.dtype != SNN_F16)
+        return fail(s, SNN_EINVAL, "%s: unknown element type %d", name, t.dtype);
+    if (type >= 0 && t.dtype != type)
+        return fail(s, SNN_EINVAL, "%s: element type %d where the others have %d", name, t.dtype, type);
+    const size_t size = t.dtype == SNN_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(t.data) % size) return fail(s, SNN_EINVAL, "%s: misaligned data", name);
+    if ((T > 1 && t.row < n) || t.row < 0 || t.sample < 0)
+        return fail(s, SNN_EINVAL, "%s: strides %lld, %lld of %d channels", name, (long long)t.row,
+                    (long long)t.sample, n);
+    out->row = t.row;
+    out->sample = t.sample;
+    return SNN_OK;
+}
+
+// An output's rows must not lie on one another.
+int out_arg(snn_seq* s, const snn_tensor& t, const char* name, int n, int T, int type, SeqT* out) {
+    const int rc = seq_arg(s, t, name, n, T, type, false, out);
+    if (rc) return rc;
+    // rows inside samples, or samples inside rows
+    const bool inside = t.sample >= (long long)(T - 1) * t.row + n;
+    const bool across = T == 1 || (t.sample >= n && t.row >= (long long)(s->o.batch - 1) * t.sample + n);
+    if (s->o.batch > 1 && !inside && !across)
+        return fail(s, SNN_EINVAL, "%s: strides %lld, %lld put rows of an output on one another", name,
+                    (long long)t.row, (long long)t.sample);
+    return SNN_OK;
+}
+
+int f32_arg(snn_seq* s, const void* p, const char* name, bool need) {
+    if (!p && need) return fail(s, SNN_EINVAL, "%s: NULL", name);
+    if (reinterpret_cast<uintptr_t>(p) % 4) return fail(s, SNN_EINVAL, "%s: misaligned", name);
+    return SNN_OK;
+}
+
+#define ARG(expr)                \
+    do {                         \
+        const int rc_ = (expr);  \
+        if (rc_) return rc_;     \
+    } while (0)
+
+void scan_sizes(const snn_seq* s, ScanArgs* k) {
+    k->batch = s->o.batch;
+    k->T = s->o.T;
+    k->channels = s->o.channels;
+    k->state = s->o.state;
+    k->groups = s->o.groups;
+    k->per = s->o.channels / s->o.groups;
+    k->gblocks = s->gblocks;
+    k->chunks = s->parts;
+    k->chunk_len = s->part_len;
+    k->segs = s->segs;
+    k->carry = s->carry;
+    k->dsum = s->dsum;
+    k->bcpart = s->bcpart;
+    k->apart = s->apart;
+    k->dpart = s->dpart;
+}
+
+}  // namespace
+
+extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
+    g_seq_err[0] = 0;
+    if (!out) return create_fail(SNN_EINVAL, "NULL out", nullptr);
+    *out = nullptr;
+    if (!o) return create_fail(SNN_EINVAL, "NULL opts", nullptr);
+    if (o->batch < 1 || o->batch > 65535) return create_fail(SNN_EINVAL, "batch must be 1 .. 65535", nullptr);
+    if (o->T < 1 || o->T > SNN_MAX_T) return create_fail(SNN_EINVAL, "T must be 1 .. SNN_MAX_T", nullptr);
+    if ((long long)o->batch * o->T > (1ll << 31)) return create_fail(SNN_EINVAL, "batch x T exceeds 2^31", nullptr);
+    if (o->channels < 1 || o->channels > SNN_SEQ_MAX_CHANNELS)
+        return create_fail(SNN_EINVAL, "channels must be 1 .. SNN_SEQ_MAX_CHANNELS", nullptr);
+    if (o->state < 1 || o->state > SNN_SEQ_MAX_STATE)
+        return create_fail(SNN_EINVAL, "state must be 1 .. SNN_SEQ_MAX_STATE", nullptr);
+    if (o->groups < 1 || o->channels % o->groups)
+        return create_fail(SNN_EINVAL, "groups must divide channels", nullptr);
+    if (o->taps < 1 || o->taps > SNN_SEQ_MAX_TAPS)
+        return create_fail(SNN_EINVAL, "taps must be 1 .. SNN_SEQ_MAX_TAPS", nullptr);
+    if (o->flags & ~(SNN_SEQ_TRAIN | SNN_SEQ_RECOMPUTE)) return create_fail(SNN_EINVAL, "unknown flags", nullptr);
+    if (o->flags == SNN_SEQ_RECOMPUTE)
+        return create_fail(SNN_EINVAL, "SNN_SEQ_RECOMPUTE goes with SNN_SEQ_TRAIN", nullptr);
+    const int np = scan_np(o->state), cb = scan_cb(np);
+    const int gblocks = (o->channels / o->groups + cb - 1) / cb;
+    const long long wgs = (long long)o->batch * o->groups * gblocks;
+    if (wgs > 0x7fffffffll / 2) return create_fail(SNN_EINVAL, "batch x channel blocks exceed a launch", nullptr);
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return create_fail(SNN_EDEVICE, "hipGetDevice", hipGetErrorString(e));
+    snn_seq* s = static_cast<snn_seq*>(calloc(1, sizeof(snn_seq)));
+    if (!s) return create_fail(SNN_ENOMEM, "out of host memory", nullptr);
+    s->o = *o;
+    s->stream = static_cast<hipStream_t>(o->hip_stream);
+    s->device = dev;
+    s->np = np;
+    s->gblocks = gblocks;
+    s->segs = (o->T + kScanSeg - 1) / kScanSeg;
+    time_parts(o->T, wgs, &s->parts, &s->part_len);
+    // floats: the parts' carries; for training the shares of the gradients
+    const bool train = o->flags & SNN_SEQ_TRAIN;
+    const size_t bp = (size_t)o->batch * s->parts, C = o->channels;
+    const size_t n_carry = s->parts > 1 ? bp * C * np : 0, n_dsum = s->parts > 1 ? bp * C : 0;
+    const size_t n_a = train ? bp * C * np : 0, n_d = train ? bp * 2 * C : 0;
+    const size_t n_bc = train ? (size_t)o->batch * o->T * o->groups * gblocks * 2 * np : 0;
+    const size_t n_conv = train ? (size_t)o->batch * conv_tiles(o->T) * (o->taps + 1) * C : 0;
+    auto round4 = [](size_t x) { return (x + 3) & ~(size_t)3; };
+    const size_t n_states = o->flags & SNN_SEQ_RECOMPUTE ? (size_t)o->batch * s->segs * C * np : 0;
+    const size_t n_scan = round4(n_carry) + round4(n_dsum) + round4(n_a) + round4(n_d) + round4(n_bc) + n_states;
+    const size_t total = std::max(n_scan, n_conv) * sizeof(float);
+    if (total) {
+        e = hipMalloc(reinterpret_cast<void**>(&s->mem), total);
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            free(s);
+            return create_fail(e == hipErrorOutOfMemory ? SNN_ENOMEM : SNN_EDEVICE, "hipMalloc", hipGetErrorString(e));
+        }
+        float* p = reinterpret_cast<float*>(s->mem);
+        s->cpart = p;                  // a call at a time uses the memory
+        s->carry = p, p += round4(n_carry);
+        s->dsum = p, p += round4(n_dsum);
+        s->apart = p, p += round4(n_a);
+        s->dpart = p, p += round4(n_d);
+        s->bcpart = p, p += round4(n_bc);
+        s->states = p;
+    }
+    *out = s;
+    return SNN_OK;
+}
+
+extern "C" const char* snn_seq_last_error(const snn_seq* s) { return s ? s->err : g_seq_err; }
+
+extern "C" void snn_seq_destroy(snn_seq* s) {
+    if (!s) return;
+    {
+        OnDevice on(s->device);
+        (void)hipStreamSynchronize(s->stream);
+        if (s->mem) (void)hipFree(s->mem);
+    }
+    free(s);
+}
+
+// ------------------------------------------------------------------ counts
+
+static int bin(snn_seq* s, BinArgs& a, int n, int factor, const snn_tensor* dst) {
+    if (!dst) return fail(s, SNN_EINVAL, "NULL dst");
+    if (n < 1 || n > SNN_MAX_INPUT) return fail(s, SNN_EINVAL, "n must be 1 .. SNN_MAX_INPUT");
+    if (factor < 1 || factor > s->o.T || factor > 65535)
+        return fail(s, SNN_EINVAL, "factor must be 1 .. T and at most 65535");
+    a.batch = s->o.batch;
+    a.T = s->o.T;
+    a.n = n;
+    a.factor = factor;
+    a.rows = (s->o.T + factor - 1) / factor;
+    ARG(out_arg(s, *dst, "dst", n, a.rows, -1, &a.y));
+    // rows a workgroup: 16 KiB of counts, so that several workgroups share a CU, or one row
+    a.tile = std::min(a.rows, std::max(1, 8192 / n));
+    SEQ_TRY(s, launch_bin(a, dst->dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_bin_spikes(snn_seq* s, const snn_spikes_in* in, int32_t n, int32_t factor,
+                                  const snn_tensor* dst) {
+    SEQ_ENTER(s);
+    if (!in || !in->offsets || in->nnz < 0 || (in->nnz > 0 && (!in->step || !in->neuron)))
+        return fail(s, SNN_EINVAL, "NULL or negative input spike list");
+    BinArgs a{};
+    a.offsets = in->offsets;
+    a.step = in->step;
+    a.neuron = in->neuron;
+    a.nnz = in->nnz;
+    return bin(s, a, n, factor, dst);
+}
+
+extern "C" int snn_seq_bin_records(snn_seq* s, const snn_spikes_out* rec, int32_t capacity, int32_t n,
+                                   int32_t factor, const snn_tensor* dst) {
+    SEQ_ENTER(s);
+    if (!rec || !rec->count || capacity < 0 || (capacity > 0 && (!rec->step || !rec->neuron)))
+        return fail(s, SNN_EINVAL, "NULL records or negative capacity");
+    BinArgs a{};
+    a.count = rec->count;
+    a.step = rec->step;
+    a.neuron = rec->neuron;
+    a.capacity = capacity;
+    return bin(s, a, n, factor, dst);
+}
+
+// ------------------------------------------------------------------ packed form
+
+static int pack_args(snn_seq* s, int n, const snn_tensor* x, const snn_tensor* q, bool to, PackArgs* a) {
+    if (!x || !q) return fail(s, SNN_EINVAL, "NULL sequence");
+    if (n < 1 || n > SNN_SEQ_MAX_CHANNELS) return fail(s, SNN_EINVAL, "n must be 1 .. SNN_SEQ_MAX_CHANNELS");
+    if (q->dtype != SNN_E4M3) return fail(s, SNN_EINVAL, "q: the packed form has type SNN_E4M3");
+    SeqT qs;
+    ARG(to ? seq_arg(s, *x, "x", n, s->o.T, -1, false, &a->x) : out_arg(s, *x, "x", n, s->o.T, -1, &a->x));
+    ARG(seq_arg(s, *q, "q", n, s->o.T, -1, true, &qs));
+    ARG(f32_arg(s, q->scale, "q.scale", true));
+    a->q = reinterpret_cast<unsigned char*>(qs.p);
+    a->scale = q->scale;
+    a->batch = s->o.batch;
+    a->T = s->o.T;
+    a->n = n;
+    if ((long long)a->batch * a->T * ((n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK) > (1ll << 34))
+        return fail(s, SNN_EINVAL, "batch x T x n exceeds a launch");
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_pack(snn_seq* s, int32_t n, const snn_tensor* x, const snn_tensor* q) {
+    SEQ_ENTER(s);
+    PackArgs a{};
+    ARG(pack_args(s, n, x, q, true, &a));
+    SEQ_TRY(s, launch_pack(a, x->dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_unpack(snn_seq* s, int32_t n, const snn_tensor* q, const snn_tensor* x) {
+    SEQ_ENTER(s);
+    PackArgs a{};
+    ARG(pack_args(s, n, x, q, false, &a));
+    SEQ_TRY(s, launch_unpack(a, x->dtype, s->stream));
+    return SNN_OK;
+}
+
+// ------------------------------------------------------------------ convolution
+
+static int conv_args(snn_seq* s, const snn_seq_conv* c, int T, ConvArgs* a) {
+    if (!c) return fail(s, SNN_EINVAL, "NULL arguments");
+    const int C = s->o.channels, type = c->x.dtype;
+    ARG(seq_arg(s, c->x, "x", C, T, -1, false, &a->x));
+    ARG(out_arg(s, c->y, "y", C, T, type, &a->y));
+    ARG(f32_arg(s, c->w, "w", true));
+    ARG(f32_arg(s, c->bias, "bias", false));
+    ARG(f32_arg(s, c->lengths, "lengths", false));
+    a->w = c->w;
+    a->bias = c->bias;
+    a->lengths = c->lengths;
+    a->state = static_cast<const char*>(c->state);
+    a->state_out = static_cast<char*>(c->state_out);
+    a->batch = s->o.batch;
+    a->T = T;
+    a->channels = C;
+    a->taps = s->o.taps;
+    a->silu = c->silu != 0;
+    a->tiles = conv_tiles(T);
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_conv_forward(snn_seq* s, const snn_seq_conv* c) {
+    SEQ_ENTER(s);
+    ConvArgs a{};
+    ARG(conv_args(s, c, s->o.T, &a));
+    if (a.state_out && a.state_out == a.state) return fail(s, SNN_EINVAL, "state_out is state");
+    SEQ_TRY(s, launch_conv_forward(a, c->x.dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_conv_step(snn_seq* s, const snn_seq_conv* c) {
+    SEQ_ENTER(s);
+    ConvArgs a{};
+    ARG(conv_args(s, c, 1, &a));
+    if (a.lengths) return fail(s, SNN_EINVAL, "lengths: a step has none");
+    SEQ_TRY(s, launch_conv_step(a, c->x.dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_conv_backward(snn_seq* s, const snn_seq_conv_grad* c) {
+    SEQ_ENTER(s);
+    if (!c) return fail(s, SNN_EINVAL, "NULL arguments");
+    if (!(s->o.flags & SNN_SEQ_TRAIN)) return fail(s, SNN_EINVAL, "the handle was made without SNN_SEQ_TRAIN");
+    const int C = s->o.channels, T = s->o.T, type = c->dy.dtype;
+    ConvArgs a{};
+    ARG(seq_arg(s, c->dy, "dy", C, T, -1, false, &a.dy));
+    ARG(seq_arg(s, c->x, "x", C, T, c->x.dtype == SNN_E4M3 ? -1 : type, true, &a.x));
+    ARG(out_arg(s, c->dx, "dx", C, T, type, &a.dx));
+    ARG(f32_arg(s, c->w, "w", true));
+    ARG(f32_arg(s, c->bias, "bias", false));
+    ARG(f32_arg(s, c->dw, "dw", true));
+    ARG(f32_arg(s, c->dbias, "dbias", false));
+    ARG(f32_arg(s, c->lengths, "lengths", false));
+    a.w = c->w;
+    a.bias = c->bias;
+    a.dw = c->dw;
+    a.dbias = c->dbias;
+    a.lengths = c->lengths;
+    a.state = static_cast<const char*>(c->state);
+    a.dstate_out = static_cast<const char*>(c->dstate_out);
+    a.dstate = static_cast<char*>(c->dstate);
+    a.batch = s->o.batch;
+    a.T = T;
+    a.channels = C;
+    a.taps = s->o.taps;
+    a.silu = c->silu != 0;
+    a.tiles = conv_tiles(T);
+    a.part = s->cpart;
+    SEQ_TRY(s, launch_conv_backward(a, type, s->stream));
+    return SNN_OK;
+}
+
+// ------------------------------------------------------------------ scan
+
+static int scan_args(snn_seq* s, const snn_seq_scan* c, int T, ScanArgs* a) {
+    if (!c) return fail(s, SNN_EINVAL, "NULL arguments");
+    const int C = s->o.channels, GN = s->o.groups * s->o.state, type = c->u.dtype;
+    ARG(seq_arg(s, c->u, "u", C, T, -1, false, &a->u));
+    ARG(seq_arg(s, c->delta, "delta", C, T, type, false, &a->delta));
+    ARG(seq_arg(s, c->B, "B", GN, T, type, false, &a->B));
+    ARG(seq_arg(s, c->C, "C", GN, T, type, false, &a->C));
+    if (c->z.data) ARG(seq_arg(s, c->z, "z", C, T, type, false, &a->z));
+    ARG(out_arg(s, c->y, "y", C, T, type, &a->y));
+    ARG(f32_arg(s, c->A, "A", true));
+    ARG(f32_arg(s, c->D, "D", false));
+    ARG(f32_arg(s, c->delta_bias, "delta_bias", false));
+    ARG(f32_arg(s, c->h0, "h0", false));
+    ARG(f32_arg(s, c->hT, "hT", false));
+    ARG(f32_arg(s, c->lengths, "lengths", false));
+    if (reinterpret_cast<uintptr_t>(c->saved) % 16) return fail(s, SNN_EINVAL, "saved: misaligned");
+    a->A = c->A;
+    a->D = c->D;
+    a->delta_bias = c->delta_bias;
+    a->h0 = c->h0;
+    a->hT = c->hT;
+    a->saved = c->saved;
+    a->lengths = c->lengths;
+    a->softplus = c->softplus != 0;
+    scan_sizes(s, a);
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_scan_forward(snn_seq* s, const snn_seq_scan* c) {
+    SEQ_ENTER(s);
+    ScanArgs a{};
+    ARG(scan_args(s, c, s->o.T, &a));
+    if (a.hT && a.hT == a.h0) return fail(s, SNN_EINVAL, "hT is h0");
+    SEQ_TRY(s, launch_scan_forward(a, c->u.dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_scan_step(snn_seq* s, const snn_seq_scan* c) {
+    SEQ_ENTER(s);
+    ScanArgs a{};
+    ARG(scan_args(s, c, 1, &a));
+    if (!a.hT) return fail(s, SNN_EINVAL, "hT: NULL");
+    if (a.lengths || a.saved) return fail(s, SNN_EINVAL, "lengths, saved: a step has none");
+    SEQ_TRY(s, launch_scan_step(a, c->u.dtype, s->stream));
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_saved(const snn_seq* s, int64_t* floats) {
+    if (!s || !floats) return SNN_EINVAL;
+    *floats = (int64_t)s->o.batch * s->segs * s->o.channels * s->np;
+    return SNN_OK;
+}
+
+extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
+    SEQ_ENTER(s);
+    if (!c) return fail(s, SNN_EINVAL, "NULL arguments");
+    if (!(s->o.flags & SNN_SEQ_TRAIN)) return fail(s, SNN_EINVAL, "the handle was made without SNN_SEQ_TRAIN");
+    const int C = s->o.channels, GN = s->o.groups * s->o.state, T = s->o.T, type = c->dy.dtype;
+    ScanArgs a{};
+    auto in = [&](const snn_tensor& t, const char* name, SeqT* to) {
+        return seq_arg(s, t, name, C, T, t.dtype == SNN_E4M3 ? -1 : type, true, to);
+    };
+    ARG(seq_arg(s, c->dy, "dy", C, T, -1, false, &a.dy));
+    ARG(in(c->u, "u", &a.u));
+    ARG(in(c->delta, "delta", &a.delta));
+    ARG(seq_arg(s, c->B, "B", GN, T, type, false, &a.B));
+    ARG(seq_arg(s, c->C, "C", GN, T, type, false, &a.C));
+    if (!c->z.data != !c->dz.data) return fail(s, SNN_EINVAL, "z and dz: one of them is NULL");
+    if (c->z.data) {
+        ARG(in(c->z, "z", &a.z));
+        ARG(out_arg(s, c->dz, "dz", C, T, type, &a.dz));
+    }
+    ARG(out_arg(s, c->du, "du", C, T, type, &a.du));
+    ARG(out_arg(s, c->ddelta, "ddelta", C, T, type, &a.ddelta));
+    ARG(out_arg(s, c->dB, "dB", GN, T, type, &a.dB));
+    ARG(out_arg(s, c->dC, "dC", GN, T, type, &a.dC));
+    ARG(f32_arg(s, c->A, "A", true));
+    ARG(f32_arg(s, c->D, "D", false));
+    ARG(f32_arg(s, c->delta_bias, "delta_bias", false));
+    ARG(f32_arg(s, c->dhT, "dhT", false));
+    ARG(f32_arg(s, c->dA, "dA", true));
+    ARG(f32_arg(s, c->dD, "dD", false));
+    ARG(f32_arg(s, c->ddelta_bias, "ddelta_bias", false));
+    ARG(f32_arg(s, c->dh0, "dh0", false));
+    ARG(f32_arg(s, c->lengths, "lengths", false));
+    ARG(f32_arg(s, c->h0, "h0", false));
+    if (!c->saved && !(s->o.flags & SNN_SEQ_RECOMPUTE))
+        return fail(s, SNN_EINVAL, "saved: NULL, and the handle was made without SNN_SEQ_RECOMPUTE");
+    if (reinterpret_cast<uintptr_t>(c->saved) % 16) return fail(s, SNN_EINVAL, "saved: misaligned");
+    a.A = c->A;
+    a.D = c->D;
+    a.delta_bias = c->delta_bias;
+    a.dhT = c->dhT;
+    a.h0 = c->h0;
+    a.saved = c->saved ? const_cast<float*>(c->saved) : s->states;
+    a.dA = c->dA;
+    a.dD = c->dD;
+    a.ddelta_bias = c->ddelta_bias;
+    a.dh0 = c->dh0;
+    a.lengths = c->lengths;
+    a.softplus = c->softplus != 0;
+    scan_sizes(s, &a);
+    if (!c->saved) SEQ_TRY(s, launch_scan_states(a, type, s->stream));
+    SEQ_TRY(s, launch_scan_backward(a, type, s->stream));
+    return SNN_OK;
+}
+
+// ------------------------------------------------------------------ sampling
+
+struct snn_sampler {
+    int rows, n, device;
+    hipStream_t stream;
+    char err[512];
+};
+
+namespace {
+int fail(snn_sampler* s, int code, const char* what, const char* why) {
+    snprintf(s->err, sizeof s->err, "%s%s%s", what, why ? ": " : "", why ? why : "");
+    return code;
+}
+}  // namespace
+
+extern "C" int snn_sampler_create(int32_t rows, int32_t n, void* hip_stream, snn_sampler** out) {
+    g_seq_err[0] = 0;
+    if (!out) return create_fail(SNN_EINVAL, "NULL out", nullptr);
+    *out = nullptr;
+    if (rows < 1) return create_fail(SNN_EINVAL, "rows must be at least 1", nullptr);
+    if (n < 1 || n > SNN_SAMPLE_MAX_N) return create_fail(SNN_EINVAL, "n must be 1 .. SNN_SAMPLE_MAX_N", nullptr);
+    int dev = 0;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return create_fail(SNN_EDEVICE, "hipGetDevice", hipGetErrorString(e));
+    snn_sampler* s = static_cast<snn_sampler*>(calloc(1, sizeof(snn_sampler)));
+    if (!s) return create_fail(SNN_ENOMEM, "out of host memory", nullptr);
+    s->rows = rows;
+    s->n = n;
+    s->device = dev;
+    s->stream = static_cast<hipStream_t>(hip_stream);
+    *out = s;
+    return SNN_OK;
+}
+
+extern "C" const char* snn_sampler_last_error(const snn_sampler* s) { return s ? s->err : g_seq_err; }
+
+extern "C" void snn_sampler_destroy(snn_sampler* s) {
+    if (!s) return;
+    {
+        OnDevice on(s->device);
+        (void)hipStreamSynchronize(s->stream);
+    }
+    free(s);
+}
+
+extern "C" int snn_sampler_sample(snn_sampler* s, const snn_sample_args* c) {
+    if (!s) return SNN_EINVAL;
+    s->err[0] = 0;
+    if (!c) return fail(s, SNN_EINVAL, "NULL arguments", nullptr);
+    if (!c->scores || !c->u || !c->token) return fail(s, SNN_EINVAL, "NULL scores, u or token", nullptr);
+    if (c->dtype != SNN_F32 && c->dtype != SNN_BF16 && c->dtype != SNN_F16)
+        return fail(s, SNN_EINVAL, "scores: unknown element type", nullptr);
+    if (reinterpret_cast<uintptr_t>(c->scores) % (c->dtype == SNN_F32 ? 4 : 2))
+        return fail(s, SNN_EINVAL, "scores: misaligned", nullptr);
+    if (c->rows < 1 || c->rows > s->rows || c->n < 1 || c->n > s->n)
+        return fail(s, SNN_EINVAL, "rows and n must be at least 1 and at most the handle's", nullptr);
+    if (c->rows > 1 && c->row < c->n) return fail(s, SNN_EINVAL, "row is below n", nullptr);
+    const void* words[] = {c->u, c->temperature, c->top_k, c->top_p, c->min_p, c->token, c->logprob};
+    for (const void* p : words)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return fail(s, SNN_EINVAL, "a misaligned array of rows", nullptr);
+    OnDevice on(s->device);
+    if (on.err != hipSuccess) return fail(s, SNN_EDEVICE, "hipSetDevice", hipGetErrorString(on.err));
+    SampleArgs a{};
+    a.scores = c->scores;
+    a.row = c->row;
+    a.rows = c->rows;
+    a.n = c->n;
+    a.shift = 62;
+    while ((1ll << (62 - a.shift)) < c->n) --a.shift;
+    a.u = c->u;
+    a.temperature = c->temperature;
+    a.top_k = c->top_k;
+    a.top_p = c->top_p;
+    a.min_p = c->min_p;
+    a.token = c->token;
+    a.logprob = c->logprob;
+    const hipError_t e = launch_sample(a, c->dtype, s->stream);
+    if (e != hipSuccess) return fail(s, SNN_EDEVICE, "launch_sample", hipGetErrorString(e));
+    return SNN_OK;
+}

@@ -1,0 +1,159 @@
+// Activations in 8 bits and back, and spike lists as dense counts.
+#include "seq_device.h"
+
+namespace {
+
+// Sixteen lanes share a block of 128 channels, 8 each; a wave has four blocks.
+constexpr int kPackLanes = SNN_SEQ_BLOCK / 8;
+
+__device__ __forceinline__ float row_max(float x) {
+    x = fmaxf(x, dpp_f32<kQuadXor1>(x));
+    x = fmaxf(x, dpp_f32<kQuadXor2>(x));
+    x = fmaxf(x, dpp_f32<kHalfMirror>(x));
+    return fmaxf(x, dpp_f32<kMirror>(x));
+}
+
+// The exponent k of the scale 2^k: the least with m <= 448 2^k = 0.875 2^(k + 9).
+__device__ __forceinline__ int scale_exp(float m) {
+    if (m == 0.0f) return 0;
+    int e;
+    const float f = frexpf(m, &e);              // m = f 2^e, 0.5 <= f < 1
+    const int k = f > 0.875f ? e - 8 : e - 9;
+    return k < -126 ? -126 : k;
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
+    const int blocks = (a.n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK;
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / kPackLanes;
+    if (i >= (long long)a.batch * a.T * blocks) return;        // whole rows of 16 lanes
+    const long long bt = i / blocks;
+    const int blk = (int)(i % blocks);
+    const int c = blk * SNN_SEQ_BLOCK + (threadIdx.x % kPackLanes) * 8, n = a.n - c;
+    Raw<T, 8, false> r;
+    float x[8], m = 0.0f;
+    raw_load(r, a.x, bt / a.T, bt % a.T, a.T, c, n);
+    raw_get(r, a.x, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float v = fabsf(x[j]);
+        m = v < INFINITY ? fmaxf(m, v) : m;
+    }
+    const int k = scale_exp(row_max(m));
+    unsigned w[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // e4m3 has no infinity
+        x[j] = fabsf(x[j]) < INFINITY ? ldexpf(x[j], -k) : NAN;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h], x[4 * h + 1], 0, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2], x[4 * h + 3], v, true);
+        w[h] = (unsigned)v;
+    }
+    unsigned char* q = a.q + bt * a.n + c;
+    if (n >= 8) {
+        typedef unsigned U2 __attribute__((ext_vector_type(2), aligned(1)));
+        *reinterpret_cast<U2*>(q) = U2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) q[j] = (unsigned char)(w[j / 4] >> (8 * (j % 4)));
+    }
+    if (threadIdx.x % kPackLanes == 0) a.scale[i] = ldexpf(1.0f, k);
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) unpack_kernel(PackArgs a) {
+    const int vecs = (a.n + 7) / 8, blocks = (a.n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (long long)a.batch * a.T * vecs) return;
+    const long long bt = i / vecs;
+    const int c = (int)(i % vecs) * 8;
+    const SeqT q{reinterpret_cast<char*>(a.q), a.scale, a.n, 0, 1, blocks};
+    Raw<T, 8, true> r;
+    float x[8];
+    raw_load(r, q, bt / a.T, bt % a.T, a.T, c, a.n - c);
+    raw_get(r, q, x);
+    store_vec<T, 8>(a.x, bt / a.T, bt % a.T, c, a.n - c, x);
+}
+
+// First event of [lo, hi) whose step is not below s.
+__device__ __forceinline__ long long first_at(const int* step, long long lo, long long hi, int s) {
+    while (lo < hi) {
+        const long long mid = lo + (hi - lo) / 2;
+        if (step[mid] < s) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+// A workgroup counts `tile` rows of the output in LDS, two 16-bit counts a
+// word (a neuron has at most one spike a step, and factor <= T <= 65536 is
+// kept below 65536 by the host), and writes them out as vectors.
+template <class T>
+__global__ void __launch_bounds__(256) bin_kernel(BinArgs a) {
+    extern __shared__ unsigned cnt[];
+    __shared__ long long range[2];
+    const int b = blockIdx.y, r0 = blockIdx.x * a.tile, nr = min(a.tile, a.rows - r0);
+    const int words = (a.tile * a.n + 1) / 2;
+    if (threadIdx.x < 2) {
+        long long lo, hi;
+        if (a.offsets) {
+            lo = min(max(a.offsets[b], 0), a.nnz);
+            hi = max(lo, (long long)min(a.offsets[b + 1], a.nnz));
+        } else {
+            lo = (long long)b * a.capacity;
+            hi = lo + min(max(a.count[b], 0), a.capacity);
+        }
+        const long long s = (long long)(r0 + (threadIdx.x ? nr : 0)) * a.factor;
+        range[threadIdx.x] = s >= a.T ? hi : first_at(a.step, lo, hi, (int)s);
+    }
+    for (int i = threadIdx.x; i < words; i += 256) cnt[i] = 0;
+    __syncthreads();
+    for (long long i = range[0] + threadIdx.x; i < range[1]; i += 256) {
+        const int s = a.step[i], c = a.neuron[i];
+        const int r = s / a.factor - r0;
+        if (s >= 0 && s < a.T && r >= 0 && r < nr && c >= 0 && c < a.n) {
+            const int at = r * a.n + c;
+            atomicAdd(&cnt[at / 2], 1u << (16 * (at % 2)));
+        }
+    }
+    __syncthreads();
+    const unsigned short* half = reinterpret_cast<const unsigned short*>(cnt);
+    const int vecs = (a.n + 7) / 8;
+    for (int i = threadIdx.x; i < nr * vecs; i += 256) {
+        const int r = i / vecs, c = i % vecs * 8, n = a.n - c;
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = j < n ? (float)half[r * a.n + c + j] : 0.0f;
+        store_vec<T, 8>(a.y, b, r0 + r, c, n, o);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_pack(const PackArgs& a, int dtype, hipStream_t s) {
+    const long long n = (long long)a.batch * a.T * ((a.n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK) * kPackLanes;
+    SEQ_BY_TYPE(dtype, T, {
+        pack_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t s) {
+    const long long n = (long long)a.batch * a.T * ((a.n + 7) / 8);
+    SEQ_BY_TYPE(dtype, T, {
+        unpack_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_bin(const BinArgs& a, int dtype, hipStream_t s) {
+    const dim3 grid((a.rows + a.tile - 1) / a.tile, a.batch);
+    const size_t lds = ((size_t)a.tile * a.n + 1) / 2 * 4;
+    SEQ_BY_TYPE(dtype, T, {
+        bin_kernel<T><<<grid, 256, lds, s>>>(a);
+        return hipGetLastError();
+    });
+}

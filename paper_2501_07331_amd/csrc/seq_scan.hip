@@ -1,0 +1,321 @@
+// Selective state-space scan, forward and single step.
+//
+// A workgroup takes CB channels of one sample over one part of the time axis,
+// tile by tile of kScanTile steps.  S lanes share a channel, each holding four
+// of its states in registers, so that a step costs each lane four exponentials
+// and its share of the sum over the states is two to four DPP additions.  What
+// is elementwise in (step, channel) -- softplus, delta' u, the gate -- is done
+// once per element by all threads on 16-byte vectors before and after the
+// tile's steps, and passes through LDS.
+#include "seq_device.h"
+
+namespace {
+
+template <int S>
+struct ScanShape {
+    static constexpr int NP = 4 * S;                            // states of a channel, padded
+    static constexpr int CB = S <= 4 ? 64 : S == 8 ? 32 : 16;   // channels of a workgroup
+    static constexpr int NT = CB * S;                           // threads
+};
+
+// Staging of B and C (one of them: ONE) of a tile: [TT][2][NP] fp32 in LDS,
+// zero past the sample's steps and the states.
+template <class T, int S, int TT, bool ONE>
+struct GroupTile {
+    static constexpr int NP = ScanShape<S>::NP, NT = ScanShape<S>::NT;
+    static constexpr int W = ONE ? NP : 2 * NP, E = (TT * W + NT - 1) / NT;
+    T raw[E];
+    __device__ __forceinline__ void load(const ScanArgs& a, const SeqT& first, const SeqT& second, int b, int g, int t0,
+                                         int len, int tid) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = e * NT + tid, t = t0 + i / W, k = i % W, n = k % NP;
+            raw[e] = T(0.0f);
+            if (i < TT * W && t < len && n < a.state) {
+                const SeqT& s = k < NP ? first : second;
+                raw[e] = reinterpret_cast<const T*>(s.p)[(long long)b * s.sample + (long long)t * s.row +
+                                                         (long long)g * a.state + n];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float* bc, int tid) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = e * NT + tid;
+            if (i < TT * W) bc[i] = (float)raw[e];
+        }
+    }
+};
+
+// What a launch is for: the whole scan; only the saved states (they are
+// computed again for the backward pass); only a part's last state from zero
+// and the sum of its delta', for the join of the parts.
+enum { SCAN_ALL, SCAN_SAVE, SCAN_ENDS };
+
+// One part of the time axis of CB channels.
+template <class T, int S, int MODE>
+__global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs a) {
+    constexpr int NP = ScanShape<S>::NP, CB = ScanShape<S>::CB, NT = ScanShape<S>::NT, TT = kScanTile;
+    constexpr bool STATES = MODE != SCAN_ALL, ENDS = MODE == SCAN_ENDS;
+    constexpr int EP = TT * CB / NT;              // elements a thread
+    constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
+    __shared__ float2 ds[TT][CB];                 // (delta', delta' u); y in its first half
+    __shared__ __align__(16) float bc[TT * (STATES ? NP : 2 * NP)];
+
+    const int tid = threadIdx.x;
+    const int blk = blockIdx.x % (a.groups * a.gblocks), b = blockIdx.x / (a.groups * a.gblocks), part = blockIdx.y;
+    const int g = blk / a.gblocks, off = (blk % a.gblocks) * CB;
+    const int nc = min(CB, a.per - off), c0 = g * a.per + off;   // channels of this workgroup
+    const int len = clamp_len(a.lengths, b, a.T);
+    const int t_begin = part * a.chunk_len, t_end = min(a.T, t_begin + a.chunk_len);
+
+    // elementwise role: VW channels from ecol of the rows erow, erow + PR, ...
+    const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
+    float bias[VW], Dv[VW];
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+        bias[i] = a.delta_bias && i < en ? a.delta_bias[c0 + ecol + i] : 0.0f;
+        Dv[i] = !STATES && a.D && i < en ? a.D[c0 + ecol + i] : 0.0f;
+    }
+    // scan role: states 4 q .. 4 q + 3 of channel ch
+    const int ch = tid / S, q = tid % S;
+    const bool live = ch < nc;
+    const long long cidx = (long long)b * a.channels + c0 + ch;
+    float A2[4], h[4], dsum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int n = 4 * q + k;
+        const bool in = live && n < a.state;
+        A2[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] * kLog2e : 0.0f;
+        h[k] = 0.0f;
+        if (!ENDS && in && part == 0 && a.h0) h[k] = a.h0[cidx * a.state + n];
+    }
+    if (!ENDS && live && part > 0) {
+        const float4 v = *reinterpret_cast<const float4*>(
+            a.carry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
+        h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
+    }
+
+    Raw<T, VW, STATES> ru[NV], rd[NV], rz[NV];   // only a backward pass has packed inputs
+    GroupTile<T, S, TT, STATES> gt;
+    auto load = [&](int t0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int t = t0 + erow + v * PR;
+            const int n = t < len && t < t_end ? en : 0;
+            raw_load(ru[v], a.u, b, t, a.T, c0 + ecol, n);
+            raw_load(rd[v], a.delta, b, t, a.T, c0 + ecol, n);
+            if (!STATES && a.z.p) raw_load(rz[v], a.z, b, t, a.T, c0 + ecol, n);
+        }
+        gt.load(a, a.B, a.C, b, g, t0, min(len, t_end), tid);
+    };
+
+    load(t_begin);
+    for (int t0 = t_begin; t0 < t_end; t0 += TT) {
+        const int nv = min(TT, len - t0);         // steps of this tile inside the sample
+        float u[NV][VW], gate[NV][VW];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int r = erow + v * PR;
+            const bool in = t0 + r < len && t0 + r < t_end;
+            float d[VW], z[VW];
+            raw_get(ru[v], a.u, u[v]);
+            raw_get(rd[v], a.delta, d);
+            if (!STATES && a.z.p) raw_get(rz[v], a.z, z);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                float sig;
+                float x = d[i] + bias[i];
+                if (a.softplus) x = softplus(x, sig);
+                x = in && i < en ? x : 0.0f;
+                ds[r][ecol + i] = make_float2(x, x * u[v][i]);
+                gate[v][i] = !STATES && a.z.p ? z[i] * sigmoid(z[i]) : 1.0f;
+            }
+        }
+        gt.store(bc, tid);
+        __syncthreads();
+        if (t0 + TT < t_end) load(t0 + TT);
+
+        for (int r8 = 0; r8 < nv; r8 += 8) {
+            if (!ENDS && a.saved && r8 % kScanSeg == 0 && live)
+                *reinterpret_cast<float4*>(
+                    a.saved + (((long long)b * a.segs + (t0 + r8) / kScanSeg) * a.channels + c0 + ch) * NP + 4 * q) =
+                    make_float4(h[0], h[1], h[2], h[3]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = r8 + j;
+                const float2 d = ds[r][ch];
+                float4 Bv, Cv;
+                if constexpr (STATES) {
+                    Bv = *reinterpret_cast<const float4*>(&bc[r * NP + 4 * q]);
+                } else {
+                    Bv = *reinterpret_cast<const float4*>(&bc[r * 2 * NP + 4 * q]);
+                    Cv = *reinterpret_cast<const float4*>(&bc[r * 2 * NP + NP + 4 * q]);
+                }
+                h[0] = fmaf(exp2_fast(d.x * A2[0]), h[0], d.y * Bv.x);
+                h[1] = fmaf(exp2_fast(d.x * A2[1]), h[1], d.y * Bv.y);
+                h[2] = fmaf(exp2_fast(d.x * A2[2]), h[2], d.y * Bv.z);
+                h[3] = fmaf(exp2_fast(d.x * A2[3]), h[3], d.y * Bv.w);
+                if constexpr (ENDS) dsum += d.x;
+                if constexpr (!STATES) {
+                    float y = Cv.x * h[0];
+                    y = fmaf(Cv.y, h[1], y);
+                    y = fmaf(Cv.z, h[2], y);
+                    y = fmaf(Cv.w, h[3], y);
+                    y = lanes_sum<S>(y);
+                    // this channel's lanes, all of one wave, have read the pair
+                    if (q == 0) ds[r][ch].x = y;
+                }
+            }
+        }
+        __syncthreads();
+        if constexpr (!STATES) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int r = erow + v * PR;
+                if (t0 + r >= t_end) continue;
+                float o[VW];
+#pragma unroll
+                for (int i = 0; i < VW; ++i)
+                    o[i] = t0 + r < len ? fmaf(Dv[i], u[v][i], ds[r][ecol + i].x) * gate[v][i] : 0.0f;
+                store_vec<T, VW>(a.y, b, t0 + r, c0 + ecol, en, o);
+            }
+            __syncthreads();
+        }
+    }
+    if (!live) return;
+    if constexpr (ENDS) {
+        const long long at = ((long long)b * a.chunks + part) * a.channels + c0 + ch;
+        *reinterpret_cast<float4*>(a.carry + at * NP + 4 * q) = make_float4(h[0], h[1], h[2], h[3]);
+        if (q == 0) a.dsum[at] = dsum;
+    } else if (!STATES && part == a.chunks - 1 && a.hT) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (4 * q + k < a.state) a.hT[cidx * a.state + 4 * q + k] = h[k];
+    }
+}
+
+// The states that the parts start from, in the place of those that they end
+// in from zero: H[0] = h0, H[k + 1] = exp(A sum delta') H[k] + end[k].
+__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, int NP) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long per = (long long)a.channels * NP;
+    if (i >= a.batch * per) return;
+    const long long b = i / per;
+    const int c = (int)(i % per / NP), n = (int)(i % NP);
+    const bool in = n < a.state;
+    const float A2 = in ? a.A[(long long)c * a.state + n] * kLog2e : 0.0f;
+    float h = in && a.h0 ? a.h0[(b * a.channels + c) * a.state + n] : 0.0f;
+    for (int k = 0; k < a.chunks; ++k) {
+        const long long at = (b * a.chunks + k) * a.channels + c;
+        const float end = k + 1 < a.chunks ? a.carry[at * NP + n] : 0.0f;
+        a.carry[at * NP + n] = h;
+        if (k + 1 < a.chunks) h = fmaf(exp2_fast(a.dsum[at] * A2), h, end);
+    }
+}
+
+// One step: a lane holds four states of a channel, S lanes a channel.
+template <class T, int S>
+__global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long ch = i / S;
+    const int q = (int)(i % S);
+    const long long total = (long long)a.batch * a.channels;
+    const bool live = ch < total;
+    const long long cc = live ? ch : total - 1;
+    const int b = (int)(cc / a.channels), c = (int)(cc % a.channels), g = c / a.per;
+    auto at = [&](const SeqT& s, long long k) { return (float)reinterpret_cast<const T*>(s.p)[b * s.sample + k]; };
+    const float u = at(a.u, c);
+    float d = at(a.delta, c) + (a.delta_bias ? a.delta_bias[c] : 0.0f), sig;
+    if (a.softplus) d = softplus(d, sig);
+    const float x = d * u;
+    const long long s0 = cc * a.state + 4 * q;
+    const float* Ap = a.A + (long long)c * a.state + 4 * q;
+    const long long g0 = (long long)g * a.state + 4 * q;
+    float y = 0.0f;
+    const bool whole = a.state % 4 == 0 && 4 * q < a.state;     // a 16-byte vector of its own
+    if (whole) {
+        const float4 A4 = *reinterpret_cast<const float4*>(Ap);
+        float4 h = a.h0 ? *reinterpret_cast<const float4*>(a.h0 + s0) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        h.x = fmaf(exp2_fast(d * (A4.x * kLog2e)), h.x, x * at(a.B, g0));
+        h.y = fmaf(exp2_fast(d * (A4.y * kLog2e)), h.y, x * at(a.B, g0 + 1));
+        h.z = fmaf(exp2_fast(d * (A4.z * kLog2e)), h.z, x * at(a.B, g0 + 2));
+        h.w = fmaf(exp2_fast(d * (A4.w * kLog2e)), h.w, x * at(a.B, g0 + 3));
+        y = at(a.C, g0) * h.x;
+        y = fmaf(at(a.C, g0 + 1), h.y, y);
+        y = fmaf(at(a.C, g0 + 2), h.z, y);
+        y = fmaf(at(a.C, g0 + 3), h.w, y);
+        if (live) *reinterpret_cast<float4*>(a.hT + s0) = h;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (4 * q + k < a.state) {
+                float h = a.h0 ? a.h0[s0 + k] : 0.0f;
+                h = fmaf(exp2_fast(d * (Ap[k] * kLog2e)), h, x * at(a.B, g0 + k));
+                y = fmaf(at(a.C, g0 + k), h, y);
+                if (live) a.hT[s0 + k] = h;
+            }
+    }
+    y = lanes_sum<S>(y);
+    if (live && q == 0) {
+        if (a.D) y = fmaf(a.D[c], u, y);
+        if (a.z.p) {
+            const float z = at(a.z, c);
+            y *= z * sigmoid(z);
+        }
+        reinterpret_cast<T*>(a.y.p)[b * a.y.sample + c] = (T)y;
+    }
+}
+
+template <class T, int S, int MODE>
+hipError_t run(const ScanArgs& a, hipStream_t s) {
+    const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
+    if (a.chunks > 1) {
+        // the last part's end is nobody's start
+        scan_forward_kernel<T, S, SCAN_ENDS><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
+        const long long n = (long long)a.batch * a.channels * ScanShape<S>::NP;
+        scan_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, ScanShape<S>::NP);
+    }
+    scan_forward_kernel<T, S, MODE><<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <class T, int S>
+hipError_t forward(const ScanArgs& a, hipStream_t s) {
+    return run<T, S, SCAN_ALL>(a, s);
+}
+
+template <class T, int S>
+hipError_t states(const ScanArgs& a, hipStream_t s) {
+    return run<T, S, SCAN_SAVE>(a, s);
+}
+
+template <class T, int S>
+hipError_t step(const ScanArgs& a, hipStream_t s) {
+    const long long n = (long long)a.batch * a.channels * S;
+    scan_step_kernel<T, S><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+#define BY_STATES(np, F, ...)                    \
+    switch (np) {                                \
+        case 4: return F<T, 1>(__VA_ARGS__);     \
+        case 8: return F<T, 2>(__VA_ARGS__);     \
+        case 16: return F<T, 4>(__VA_ARGS__);    \
+        case 32: return F<T, 8>(__VA_ARGS__);    \
+        default: return F<T, 16>(__VA_ARGS__);   \
+    }
+
+hipError_t launch_scan_forward(const ScanArgs& a, int dtype, hipStream_t s) {
+    SEQ_BY_TYPE(dtype, T, BY_STATES(scan_np(a.state), forward, a, s));
+}
+
+hipError_t launch_scan_states(const ScanArgs& a, int dtype, hipStream_t s) {
+    SEQ_BY_TYPE(dtype, T, BY_STATES(scan_np(a.state), states, a, s));
+}
+
+hipError_t launch_scan_step(const ScanArgs& a, int dtype, hipStream_t s) {
+    SEQ_BY_TYPE(dtype, T, BY_STATES(scan_np(a.state), step, a, s));
+}

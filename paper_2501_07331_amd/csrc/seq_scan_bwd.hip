@@ -1,0 +1,399 @@
+// Backward pass of the selective state-space scan.
+//
+// With dy' = dy silu(z), the adjoint of the state runs in reverse,
+//   g[t] = C[t] dy'[t] + a[t + 1] g[t + 1],
+// and at every step
+//   dC = sum_c dy' h,  dB = sum_c g delta' u,  s1 = sum_n g B,
+//   s2 = sum_n g a h[t - 1] A,  dA += g a h[t - 1] delta'.
+// A tile is one segment of kScanSeg steps: its states are run again from the
+// one that the forward pass saved at its start and kept in registers with
+// their decays, then the tile is run backwards.  Lanes, tiles and the
+// elementwise work are those of the forward kernel.  The sums over channels
+// are taken in three steps of fixed order: within a wave by lane swaps, over
+// the workgroup's waves in LDS, over workgroups by scan_sums_kernel.
+#include "seq_device.h"
+
+namespace {
+
+template <int S>
+struct BwdShape {
+    static constexpr int NP = 4 * S;
+    static constexpr int CB = S <= 4 ? 64 : S == 8 ? 32 : 16;
+    static constexpr int NT = CB * S;
+    static constexpr int WAVES = NT / 64;
+};
+
+__device__ __forceinline__ void swap_add32(float& a, float b) {
+    // lower lanes: a of both halves, upper lanes: b of both halves
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    a = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap_add16(float& a, float b) {
+    // even rows of 16 lanes: a of a pair of rows, odd rows: b
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    a = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Sum over the lanes of a row of 16 that are S apart.
+template <int S>
+__device__ __forceinline__ float row_sum(float x) {
+    if constexpr (S <= 8) x += dpp_f32<kRor | 8>(x);
+    if constexpr (S <= 4) x += dpp_f32<kRor | 4>(x);
+    if constexpr (S <= 2) x += dpp_f32<kRor | 2>(x);
+    if constexpr (S <= 1) x += dpp_f32<kRor | 1>(x);
+    return x;
+}
+
+// One part of the time axis of CB channels.  STATES: only the adjoint at the
+// part's start from zero at its end, and the sum of its delta'.
+template <class T, int S, bool STATES>
+__global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs a) {
+    constexpr int NP = BwdShape<S>::NP, CB = BwdShape<S>::CB, NT = BwdShape<S>::NT, TT = kScanSeg;
+    constexpr int W = BwdShape<S>::WAVES;
+    constexpr int EP = TT * CB / NT;
+    constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
+    constexpr int BW = 2 * NP, BE = (TT * BW + NT - 1) / NT;
+    __shared__ float2 ds[TT][CB];                  // (delta', delta' u), then (s1, s2)
+    __shared__ float dyl[TT][CB];                  // dy'
+    __shared__ float yl[STATES ? 1 : TT][CB];      // sum_n C h
+    __shared__ __align__(16) float bc[TT * BW];
+    __shared__ float red[STATES ? 1 : TT][W][BW];  // the waves' shares of dB, dC
+
+    const int tid = threadIdx.x;
+    const int nblk = a.groups * a.gblocks;
+    const int blk = blockIdx.x % nblk, b = blockIdx.x / nblk, part = blockIdx.y + (STATES ? 1 : 0);
+    const int g = blk / a.gblocks, off = (blk % a.gblocks) * CB;
+    const int nc = min(CB, a.per - off), c0 = g * a.per + off;
+    const int len = clamp_len(a.lengths, b, a.T);
+    const int t_begin = part * a.chunk_len, t_end = min(a.T, t_begin + a.chunk_len);
+
+    const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
+    float bias[VW], Dv[VW], sumD[VW], sumB[VW];
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+        bias[i] = a.delta_bias && i < en ? a.delta_bias[c0 + ecol + i] : 0.0f;
+        Dv[i] = a.D && i < en ? a.D[c0 + ecol + i] : 0.0f;
+        sumD[i] = sumB[i] = 0.0f;
+    }
+    const int ch = tid / S, q = tid % S, wave = tid / 64, lane = tid % 64;
+    const bool live = ch < nc;
+    const long long cidx = (long long)b * a.channels + c0 + ch;
+    float A[4], A2[4], gr[4], dA[4], dsum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int n = 4 * q + k;
+        const bool in = live && n < a.state;
+        A[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] : 0.0f;
+        A2[k] = A[k] * kLog2e;
+        dA[k] = gr[k] = 0.0f;
+        if (!STATES && a.chunks == 1 && in && a.dhT) gr[k] = a.dhT[cidx * a.state + n];
+    }
+    if (!STATES && live && a.chunks > 1) {
+        const float4 v = *reinterpret_cast<const float4*>(
+            a.carry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
+        gr[0] = v.x, gr[1] = v.y, gr[2] = v.z, gr[3] = v.w;
+    }
+
+    const int last = t_begin + (t_end - 1 - t_begin) / TT * TT;
+    for (int t0 = last; t0 >= t_begin; t0 -= TT) {
+        if (t0 >= len) {
+            // nothing of the sample: the outputs' rows are zero
+            if constexpr (!STATES) {
+                const float zero[VW] = {};
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int t = t0 + erow + v * PR;
+                    if (t >= t_end) continue;
+                    store_vec<T, VW>(a.du, b, t, c0 + ecol, en, zero);
+                    store_vec<T, VW>(a.ddelta, b, t, c0 + ecol, en, zero);
+                    if (a.dz.p) store_vec<T, VW>(a.dz, b, t, c0 + ecol, en, zero);
+                }
+            }
+            continue;
+        }
+        float4 h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (!STATES && live)
+            h4 = *reinterpret_cast<const float4*>(
+                a.saved + (((long long)b * a.segs + t0 / TT) * a.channels + c0 + ch) * NP + 4 * q);
+        float u[NV][VW], d[NV][VW], sg[NV][VW], dy[NV][VW], z[NV][VW];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int t = t0 + erow + v * PR, n = t < len && t < t_end ? en : 0;
+            Raw<T, VW, true> r;
+            Raw<T, VW, false> rp;
+            raw_load(r, a.u, b, t, a.T, c0 + ecol, n);
+            raw_get(r, a.u, u[v]);
+            raw_load(r, a.delta, b, t, a.T, c0 + ecol, n);
+            raw_get(r, a.delta, d[v]);
+            raw_load(rp, a.dy, b, t, a.T, c0 + ecol, n);
+            raw_get(rp, a.dy, dy[v]);
+            if (a.z.p) {
+                raw_load(r, a.z, b, t, a.T, c0 + ecol, n);
+                raw_get(r, a.z, z[v]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < BE; ++e) {
+            const int i = e * NT + tid, t = t0 + i / BW, k = i % BW, n = k % NP;
+            float x = 0.0f;
+            if (i < TT * BW && t < len && t < t_end && n < a.state) {
+                const SeqT& s = k < NP ? a.B : a.C;
+                x = (float)reinterpret_cast<const T*>(s.p)[b * s.sample + t * s.row + (long long)g * a.state + n];
+            }
+            if (i < TT * BW) bc[i] = x;
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int r = erow + v * PR;
+            const bool in = t0 + r < len && t0 + r < t_end;
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                float x = d[v][i] + bias[i], sig = 1.0f;
+                if (a.softplus) x = softplus(x, sig);
+                x = in && i < en ? x : 0.0f;
+                d[v][i] = x;
+                sg[v][i] = sig;
+                ds[r][ecol + i] = make_float2(x, x * u[v][i]);
+                const float gate = a.z.p ? z[v][i] * sigmoid(z[v][i]) : 1.0f;
+                dyl[r][ecol + i] = dy[v][i] * gate;
+            }
+        }
+        __syncthreads();
+
+        if constexpr (STATES) {
+#pragma unroll
+            for (int r = TT - 1; r >= 0; --r) {
+                const float2 x = ds[r][ch];
+                const float dyp = dyl[r][ch];
+                const float4 Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
+                gr[0] = exp2_fast(x.x * A2[0]) * fmaf(Cv.x, dyp, gr[0]);
+                gr[1] = exp2_fast(x.x * A2[1]) * fmaf(Cv.y, dyp, gr[1]);
+                gr[2] = exp2_fast(x.x * A2[2]) * fmaf(Cv.z, dyp, gr[2]);
+                gr[3] = exp2_fast(x.x * A2[3]) * fmaf(Cv.w, dyp, gr[3]);
+                dsum += x.x;
+            }
+        } else {
+            // the states before each step, and the decays
+            float h[TT + 1][4], dec[TT][4];
+            h[0][0] = h4.x, h[0][1] = h4.y, h[0][2] = h4.z, h[0][3] = h4.w;
+#pragma unroll
+            for (int r = 0; r < TT; ++r) {
+                const float2 x = ds[r][ch];
+                const float4 Bv = *reinterpret_cast<const float4*>(&bc[r * BW + 4 * q]);
+                const float Bk[4] = {Bv.x, Bv.y, Bv.z, Bv.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    dec[r][k] = exp2_fast(x.x * A2[k]);
+                    h[r + 1][k] = fmaf(dec[r][k], h[r][k], x.y * Bk[k]);
+                }
+                if (a.z.p) {
+                    const float4 Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
+                    float y = Cv.x * h[r + 1][0];
+                    y = fmaf(Cv.y, h[r + 1][1], y);
+                    y = fmaf(Cv.z, h[r + 1][2], y);
+                    y = fmaf(Cv.w, h[r + 1][3], y);
+                    y = lanes_sum<S>(y);
+                    if (q == 0) yl[r][ch] = y;
+                }
+            }
+#pragma unroll
+            for (int r = TT - 1; r >= 0; --r) {
+                const float2 x = ds[r][ch];
+                const float dyp = dyl[r][ch];
+                const float4 Bv = *reinterpret_cast<const float4*>(&bc[r * BW + 4 * q]);
+                const float4 Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
+                const float Bk[4] = {Bv.x, Bv.y, Bv.z, Bv.w}, Ck[4] = {Cv.x, Cv.y, Cv.z, Cv.w};
+                float s1 = 0.0f, s2 = 0.0f, dB[4], dC[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    gr[k] = fmaf(Ck[k], dyp, gr[k]);
+                    dB[k] = gr[k] * x.y;
+                    dC[k] = dyp * h[r + 1][k];
+                    s1 = fmaf(gr[k], Bk[k], s1);
+                    gr[k] *= dec[r][k];
+                    const float p = gr[k] * h[r][k];
+                    s2 = fmaf(p, A[k], s2);
+                    dA[k] = fmaf(p, x.x, dA[k]);
+                }
+                s1 = lanes_sum<S>(s1);
+                s2 = lanes_sum<S>(s2);
+                if (q == 0) ds[r][ch] = make_float2(s1, s2);
+                // rows of 16 lanes 0, 1: dB of states 0 1, 2 3 of the lane's four; rows 2, 3: dC
+#pragma unroll
+                for (int k = 0; k < 4; ++k) swap_add32(dB[k], dC[k]);
+                swap_add16(dB[0], dB[2]);
+                swap_add16(dB[1], dB[3]);
+                dB[0] = row_sum<S>(dB[0]);
+                dB[1] = row_sum<S>(dB[1]);
+                if (lane % 16 < S) {
+                    const int at = (lane >> 5) * NP + 4 * q + 2 * ((lane >> 4) & 1);
+                    *reinterpret_cast<float2*>(&red[r][wave][at]) = make_float2(dB[0], dB[1]);
+                }
+            }
+        }
+        __syncthreads();
+        if constexpr (!STATES) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int r = erow + v * PR, t = t0 + r;
+                if (t >= t_end) continue;
+                float du[VW], dd[VW], dz[VW];
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    const bool in = t < len && i < en;
+                    const float2 s = ds[r][ecol + i];
+                    float dyp = dy[v][i];
+                    dz[i] = 0.0f;
+                    if (a.z.p) {
+                        const float p = sigmoid(z[v][i]), y = fmaf(Dv[i], u[v][i], yl[r][ecol + i]);
+                        dz[i] = in ? dy[v][i] * y * (p * fmaf(z[v][i], 1.0f - p, 1.0f)) : 0.0f;
+                        dyp *= z[v][i] * p;
+                    }
+                    du[i] = in ? fmaf(Dv[i], dyp, d[v][i] * s.x) : 0.0f;
+                    dd[i] = in ? fmaf(u[v][i], s.x, s.y) * sg[v][i] : 0.0f;
+                    sumD[i] = in ? fmaf(dyp, u[v][i], sumD[i]) : sumD[i];
+                    sumB[i] += dd[i];
+                }
+                store_vec<T, VW>(a.du, b, t, c0 + ecol, en, du);
+                store_vec<T, VW>(a.ddelta, b, t, c0 + ecol, en, dd);
+                if (a.dz.p) store_vec<T, VW>(a.dz, b, t, c0 + ecol, en, dz);
+            }
+            for (int i = tid; i < TT * BW; i += NT) {
+                const int r = i / BW, k = i % BW;
+                float x = red[r][0][k];
+#pragma unroll
+                for (int w = 1; w < W; ++w) x += red[r][w][k];
+                if (t0 + r < t_end) a.bcpart[(((long long)b * a.T + t0 + r) * nblk + blk) * BW + k] = x;
+            }
+        }
+        __syncthreads();
+    }
+
+    const long long row = (long long)b * a.chunks + part;
+    if (live) {
+        const long long at = (row * a.channels + c0 + ch);
+        if constexpr (STATES) {
+            *reinterpret_cast<float4*>(a.carry + at * NP + 4 * q) = make_float4(gr[0], gr[1], gr[2], gr[3]);
+            if (q == 0) a.dsum[at] = dsum;
+        } else {
+            *reinterpret_cast<float4*>(a.apart + at * NP + 4 * q) = make_float4(dA[0], dA[1], dA[2], dA[3]);
+            if (part == 0 && a.dh0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (4 * q + k < a.state) a.dh0[cidx * a.state + 4 * q + k] = gr[k];
+        }
+    }
+    if constexpr (!STATES) {
+        // dD, ddelta_bias: the rows' sums in order
+        float* col = &ds[0][0].x;                  // [2][PR][CB], PR <= TT rows
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            col[erow * CB + ecol + i] = sumD[i];
+            col[(PR + erow) * CB + ecol + i] = sumB[i];
+        }
+        __syncthreads();
+        for (int i = tid; i < 2 * CB; i += NT) {
+            const int c = i % CB;
+            float x = 0.0f;
+            for (int r = 0; r < PR; ++r) x += col[(i / CB * PR + r) * CB + c];
+            if (c < nc) a.dpart[(row * 2 + i / CB) * a.channels + c0 + c] = x;
+        }
+    }
+}
+
+// The adjoints that the parts start from at their ends, in the place of those
+// at their starts from zero: from the last part, where it is dhT, downwards.
+__global__ void __launch_bounds__(256) scan_join_back_kernel(ScanArgs a, int NP) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long per = (long long)a.channels * NP;
+    if (i >= a.batch * per) return;
+    const long long b = i / per;
+    const int c = (int)(i % per / NP), n = (int)(i % NP);
+    const bool in = n < a.state;
+    const float A2 = in ? a.A[(long long)c * a.state + n] * kLog2e : 0.0f;
+    float g = in && a.dhT ? a.dhT[(b * a.channels + c) * a.state + n] : 0.0f;
+    for (int k = a.chunks - 1; k >= 0; --k) {
+        const long long at = (b * a.chunks + k) * a.channels + c;
+        const float start = k > 0 ? a.carry[at * NP + n] : 0.0f;
+        a.carry[at * NP + n] = g;
+        if (k > 0) g = fmaf(exp2_fast(a.dsum[at] * A2), g, start);
+    }
+}
+
+// The sums over workgroups.  The first blocks sum the shares of dB and dC, an
+// element a thread; the others 32 columns of dA, dD and ddelta_bias each, in
+// 8 interleaved runs of rows that are added up in order.
+template <class T>
+__global__ void __launch_bounds__(256) scan_sums_kernel(ScanArgs a, int NP, int bc_blocks) {
+    if ((int)blockIdx.x < bc_blocks) {
+        const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+        const int w = 2 * a.groups * a.state;
+        if (i >= (long long)a.batch * a.T * w) return;
+        const long long bt = i / w;
+        const int k = (int)(i % w), which = k / (a.groups * a.state), gn = k % (a.groups * a.state);
+        const int g = gn / a.state, n = gn % a.state;
+        const float* p = a.bcpart + (bt * a.groups + g) * a.gblocks * 2 * NP + which * NP + n;
+        float x = 0.0f;
+        if ((int)(bt % a.T) < clamp_len(a.lengths, (int)(bt / a.T), a.T))
+            for (int j = 0; j < a.gblocks; ++j) x += p[(long long)j * 2 * NP];
+        const SeqT& s = which ? a.dC : a.dB;
+        reinterpret_cast<T*>(s.p)[bt / a.T * s.sample + bt % a.T * s.row + gn] = (T)x;
+        return;
+    }
+    __shared__ float part[8][32];
+    const long long na = (long long)a.channels * NP, all = na + 2 * a.channels;
+    const long long col = (long long)(blockIdx.x - bc_blocks) * 32 + threadIdx.x % 32;
+    const int run = threadIdx.x / 32, rows = a.batch * a.chunks;
+    float x = 0.0f;
+    if (col < all) {
+        const float* p = col < na ? a.apart + col : a.dpart + (col - na);
+        const long long stride = col < na ? na : 2 * a.channels;
+        for (int r = run; r < rows; r += 8) x += p[r * stride];
+    }
+    part[run][threadIdx.x % 32] = x;
+    __syncthreads();
+    if (run || col >= all) return;
+#pragma unroll
+    for (int j = 1; j < 8; ++j) x += part[j][threadIdx.x];
+    if (col < na) {
+        const long long c = col / NP;
+        const int n = (int)(col % NP);
+        if (n < a.state) a.dA[c * a.state + n] = x;
+    } else if (col - na < a.channels) {
+        if (a.dD) a.dD[col - na] = x;
+    } else if (a.ddelta_bias) {
+        a.ddelta_bias[col - na - a.channels] = x;
+    }
+}
+
+template <class T, int S>
+hipError_t backward(const ScanArgs& a, hipStream_t s) {
+    constexpr int NP = BwdShape<S>::NP;
+    const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(BwdShape<S>::NT);
+    if (a.chunks > 1) {
+        // the first part's start is nobody's end
+        scan_backward_kernel<T, S, true><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
+        const long long n = (long long)a.batch * a.channels * NP;
+        scan_join_back_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, NP);
+    }
+    scan_backward_kernel<T, S, false><<<grid, block, 0, s>>>(a);
+    const long long bc = (long long)a.batch * a.T * 2 * a.groups * a.state;
+    const long long cols = (long long)a.channels * (NP + 2);
+    const int bc_blocks = (int)((bc + 255) / 256);
+    scan_sums_kernel<T><<<(unsigned)(bc_blocks + (cols + 31) / 32), 256, 0, s>>>(a, NP, bc_blocks);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+#define BY_STATES(np, F, ...)                    \
+    switch (np) {                                \
+        case 4: return F<T, 1>(__VA_ARGS__);     \
+        case 8: return F<T, 2>(__VA_ARGS__);     \
+        case 16: return F<T, 4>(__VA_ARGS__);    \
+        case 32: return F<T, 8>(__VA_ARGS__);    \
+        default: return F<T, 16>(__VA_ARGS__);   \
+    }
+
+hipError_t launch_scan_backward(const ScanArgs& a, int dtype, hipStream_t s) {
+    SEQ_BY_TYPE(dtype, T, BY_STATES(scan_np(a.state), backward, a, s));
+}

@@ -1,0 +1,432 @@
+"""Sequence operators over the networks' trials: ctypes marshalling for
+``include/snn_seq.h`` (names follow it).
+
+``SequenceLayer`` holds one handle: spike lists as dense counts, the short
+causal convolution, the selective state-space scan, and activations in 8
+bits.  ``Packed`` is the 8-bit form of an activation.  ``Sampler`` draws a
+class from each row of scores (``Network.sample`` from a network's z).  As in ``Network``, the
+caller owns every tensor; outputs are written in place and nothing is
+allocated, so that calls can be captured into graphs.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+from .binding import SNN_OK, SNNError, load_library, snn_spikes_in, snn_spikes_out
+
+SNN_F32, SNN_BF16, SNN_F16, SNN_E4M3 = 0, 1, 2, 3
+SNN_SEQ_BLOCK, SNN_SEQ_SEGMENT = 128, 16
+SNN_SEQ_MAX_CHANNELS, SNN_SEQ_MAX_STATE, SNN_SEQ_MAX_TAPS = 65536, 64, 8
+SNN_SEQ_TRAIN, SNN_SEQ_RECOMPUTE = 1, 2
+SNN_SAMPLE_MAX_N = 1 << 24
+
+P = C.c_void_p
+
+
+class snn_tensor(C.Structure):
+    _fields_ = [("data", P), ("scale", P), ("row", C.c_int64), ("sample", C.c_int64), ("dtype", C.c_int32)]
+
+
+class snn_seq_opts(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("T", C.c_int32), ("channels", C.c_int32), ("state", C.c_int32),
+                ("groups", C.c_int32), ("taps", C.c_int32), ("flags", C.c_int32), ("hip_stream", P)]
+
+
+class snn_seq_conv(C.Structure):
+    _fields_ = [("x", snn_tensor), ("y", snn_tensor), ("w", P), ("bias", P), ("lengths", P), ("state", P),
+                ("state_out", P), ("silu", C.c_int32)]
+
+
+class snn_seq_conv_grad(C.Structure):
+    _fields_ = [("x", snn_tensor), ("dy", snn_tensor), ("dx", snn_tensor), ("w", P), ("bias", P), ("dw", P),
+                ("dbias", P), ("lengths", P), ("state", P), ("dstate_out", P), ("dstate", P), ("silu", C.c_int32)]
+
+
+class snn_seq_scan(C.Structure):
+    _fields_ = [(n, snn_tensor) for n in ("u", "delta", "B", "C", "z", "y")] + \
+               [(n, P) for n in ("A", "D", "delta_bias", "h0", "hT", "saved", "lengths")] + [("softplus", C.c_int32)]
+
+
+class snn_seq_scan_grad(C.Structure):
+    _fields_ = [(n, snn_tensor) for n in ("u", "delta", "B", "C", "z", "dy", "du", "ddelta", "dB", "dC", "dz")] + \
+               [(n, P) for n in ("A", "D", "delta_bias", "h0", "dhT", "saved", "dA", "dD", "ddelta_bias", "dh0", "lengths")] + \
+               [("softplus", C.c_int32)]
+
+
+class snn_sample_args(C.Structure):
+    _fields_ = [("scores", P), ("row", C.c_int64), ("dtype", C.c_int32), ("rows", C.c_int32), ("n", C.c_int32)] + \
+               [(n, P) for n in ("u", "temperature", "top_k", "top_p", "min_p", "token", "logprob")]
+
+
+def _bind(lib):
+    if getattr(lib, "_seq_bound", False):
+        return lib
+    T = C.POINTER(snn_tensor)
+    for name, args in (
+            ("snn_seq_create", [C.POINTER(snn_seq_opts), C.POINTER(P)]),
+            ("snn_seq_bin_spikes", [P, C.POINTER(snn_spikes_in), C.c_int32, C.c_int32, T]),
+            ("snn_seq_bin_records", [P, C.POINTER(snn_spikes_out), C.c_int32, C.c_int32, C.c_int32, T]),
+            ("snn_seq_pack", [P, C.c_int32, T, T]),
+            ("snn_seq_unpack", [P, C.c_int32, T, T]),
+            ("snn_seq_conv_forward", [P, C.POINTER(snn_seq_conv)]),
+            ("snn_seq_conv_backward", [P, C.POINTER(snn_seq_conv_grad)]),
+            ("snn_seq_conv_step", [P, C.POINTER(snn_seq_conv)]),
+            ("snn_seq_scan_forward", [P, C.POINTER(snn_seq_scan)]),
+            ("snn_seq_saved", [P, C.POINTER(C.c_int64)]),
+            ("snn_seq_scan_backward", [P, C.POINTER(snn_seq_scan_grad)]),
+            ("snn_seq_scan_step", [P, C.POINTER(snn_seq_scan)]),
+            ("snn_sampler_create", [C.c_int32, C.c_int32, P, C.POINTER(P)]),
+            ("snn_sampler_sample", [P, C.POINTER(snn_sample_args)])):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = args, C.c_int
+    lib.snn_seq_last_error.argtypes, lib.snn_seq_last_error.restype = [P], C.c_char_p
+    lib.snn_seq_destroy.argtypes, lib.snn_seq_destroy.restype = [P], None
+    lib.snn_sampler_last_error.argtypes, lib.snn_sampler_last_error.restype = [P], C.c_char_p
+    lib.snn_sampler_destroy.argtypes, lib.snn_sampler_destroy.restype = [P], None
+    lib._seq_bound = True
+    return lib
+
+
+_TYPES = None
+
+
+def _dtype(t) -> int:
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: SNN_F32, torch.bfloat16: SNN_BF16, torch.float16: SNN_F16}
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError(f"a sequence must be float32, bfloat16 or float16, got {t.dtype}") from None
+
+
+class Packed:
+    """An activation [batch][T][n] in 8 bits: ``data`` (uint8, e4m3) and
+    ``scale`` (fp32, [batch][T][ceil(n / 128)], powers of two)."""
+
+    def __init__(self, data, scale):
+        import torch
+        if data.dim() != 3 or data.dtype != torch.uint8 or not data.is_contiguous():
+            raise ValueError("data must be a contiguous uint8 [batch][T][n] tensor")
+        want = (data.shape[0], data.shape[1], -(-data.shape[2] // SNN_SEQ_BLOCK))
+        if tuple(scale.shape) != want or scale.dtype != torch.float32 or not scale.is_contiguous():
+            raise ValueError(f"scale must be a contiguous float32 {list(want)} tensor")
+        if data.device != scale.device:
+            raise ValueError("data and scale must be on one device")
+        self.data, self.scale = data, scale
+
+    @classmethod
+    def like(cls, x) -> "Packed":
+        """Memory for the packed form of x."""
+        import torch
+        B, T, n = x.shape
+        return cls(torch.empty(B, T, n, dtype=torch.uint8, device=x.device),
+                   torch.empty(B, T, -(-n // SNN_SEQ_BLOCK), dtype=torch.float32, device=x.device))
+
+    @property
+    def shape(self):
+        return self.data.shape
+
+    @property
+    def device(self):
+        return self.data.device
+
+
+class _Handle:
+    """What the handles share: their stream and device, and the checks of
+    tensors.  A call made while another stream is current waits for that
+    stream's work, and that stream for the call's."""
+
+    _destroy = None
+
+    def _open(self, stream):
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        self.stream = stream
+        self.device = stream.device
+
+    def _f32(self, t, numel, name, need=False):
+        import torch
+        return self._vec(t, torch.float32, numel, name, need)
+
+    def _vec(self, t, dtype, numel, name, need=False):
+        if t is None:
+            if need:
+                raise ValueError(f"{name} is needed")
+            return None
+        self._on_device(t, name)
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.numel() != numel:
+            raise ValueError(f"{name} must hold {numel} elements, got {t.numel()}")
+        return C.c_void_p(t.data_ptr()) if numel else None
+
+    def _on_device(self, t, name):
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
+
+    def _call(self, f, *args):
+        import torch
+        cur = torch.cuda.current_stream(self.device)
+        other = cur.cuda_stream != self.stream.cuda_stream
+        if other:
+            if self.stream.cuda_stream == 0 and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the handle is bound to the default stream, which cannot be captured: "
+                                   "make it under the stream of the capture")
+            self.stream.wait_stream(cur)
+        rc = f(self._h, *args)
+        if other:
+            cur.wait_stream(self.stream)
+        if rc != SNN_OK:
+            raise SNNError(rc, self._error(self._h).decode())
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class SequenceLayer(_Handle):
+    """One snn_seq handle: the operators for `batch` samples of `T` steps and
+    `channels` channels, bound to the current torch stream at creation.
+
+    Sequences are [batch][T][n] tensors of float32, bfloat16 or float16 whose
+    last dimension is contiguous; the others may be strided (parts of a wider
+    tensor).  Parameters, states and their gradients are contiguous float32,
+    the convolution's states of the sequences' type.  ``train``: the backward
+    passes will be called (their scratch is allocated here); ``recompute``:
+    scan_backward will be called without saved states."""
+
+    def __init__(self, batch: int, T: int, channels: int, state: int = 16, groups: int = 1, taps: int = 4,
+                 train: bool = False, recompute: bool = False, stream=None):
+        import torch
+        self._lib = _bind(load_library())
+        self._destroy, self._error = self._lib.snn_seq_destroy, self._lib.snn_seq_last_error
+        self.batch, self.T, self.channels = int(batch), int(T), int(channels)
+        self.state, self.groups, self.taps = int(state), int(groups), int(taps)
+        self.train = bool(train)
+        self._open(stream)
+        opts = snn_seq_opts(self.batch, self.T, self.channels, self.state, self.groups, self.taps,
+                            (SNN_SEQ_TRAIN if train else 0) | (SNN_SEQ_RECOMPUTE if recompute else 0), C.c_void_p(self.stream.cuda_stream))
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = self._lib.snn_seq_create(C.byref(opts), C.byref(h))
+        if rc != SNN_OK:
+            raise SNNError(rc, f"snn_seq_create failed ({self._lib.snn_seq_last_error(None).decode()})")
+        self._h = h
+        n = C.c_int64()
+        self._lib.snn_seq_saved(h, C.byref(n))
+        #: shape of scan_forward's ``saved``: a state of each channel every 16 steps
+        self.saved_shape = (self.batch, -(-self.T // SNN_SEQ_SEGMENT), self.channels,
+                            n.value // (self.batch * -(-self.T // SNN_SEQ_SEGMENT) * self.channels))
+
+    # ---------------------------------------------------------------- arguments
+
+    def _seq(self, t, name, n, rows=None, packed=False, need=True):
+        """A sequence argument; rows None: T, 0: a step's [batch][n]."""
+        if t is None:
+            if need:
+                raise ValueError(f"{name} is needed")
+            return snn_tensor()
+        rows = self.T if rows is None else rows
+        if isinstance(t, Packed):
+            if not packed:
+                raise ValueError(f"{name} must not be packed here")
+            if tuple(t.shape) != (self.batch, rows, n):
+                raise ValueError(f"{name} must be {[self.batch, rows, n]}, got {list(t.shape)}")
+            self._on_device(t, name)
+            return snn_tensor(t.data.data_ptr(), t.scale.data_ptr(), n, n * rows, SNN_E4M3)
+        self._on_device(t, name)
+        want = (self.batch, rows, n) if rows else (self.batch, n)
+        if tuple(t.shape) != want:
+            raise ValueError(f"{name} must be {list(want)}, got {list(t.shape)}")
+        if t.stride(-1) != 1 and n > 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+        return snn_tensor(t.data_ptr(), None, t.stride(1) if rows else n, t.stride(0), _dtype(t))
+
+    def _lengths(self, lengths):
+        import torch
+        return self._vec(lengths, torch.int32, self.batch, "lengths")
+
+    # ---------------------------------------------------------------- counts
+
+    def bin_spikes(self, offsets, step, neuron, dst, factor: int = 1):
+        """Counts of an input spike list (Network.forward's offsets, step,
+        neuron) in bins of `factor` steps: dst [batch][ceil(T / factor)][n]."""
+        import torch
+        inp = snn_spikes_in(self._vec(offsets, torch.int32, self.batch + 1, "offsets", True),
+                            self._vec(step, torch.int32, neuron.numel(), "step", True),
+                            self._vec(neuron, torch.int32, neuron.numel(), "neuron", True), neuron.numel())
+        d = self._binned(dst, factor)
+        self._call(self._lib.snn_seq_bin_spikes, C.byref(inp), dst.shape[-1], int(factor), C.byref(d))
+
+    def bin_records(self, count, step, neuron, dst, factor: int = 1):
+        """The same of one layer's spike records (count [batch], step and
+        neuron [batch][capacity])."""
+        import torch
+        if step.dim() != 2 or step.shape[0] != self.batch:
+            raise ValueError("step must be [batch][capacity]")
+        rec = snn_spikes_out(self._vec(count, torch.int32, self.batch, "count", True),
+                             self._vec(step, torch.int32, step.numel(), "step", True),
+                             self._vec(neuron, torch.int32, step.numel(), "neuron", True))
+        d = self._binned(dst, factor)
+        self._call(self._lib.snn_seq_bin_records, C.byref(rec), step.shape[1], dst.shape[-1], int(factor), C.byref(d))
+
+    def _binned(self, dst, factor):
+        if factor < 1 or factor > self.T:
+            raise ValueError(f"factor must be 1 .. {self.T}")
+        return self._seq(dst, "dst", dst.shape[-1], rows=-(-self.T // int(factor)))
+
+    # ---------------------------------------------------------------- packed form
+
+    def pack(self, x, q: Packed):
+        """q: the 8-bit form of x [batch][T][n] (any n)."""
+        n = x.shape[-1]
+        a, b = self._seq(x, "x", n), self._seq(q, "q", n, packed=True)
+        self._call(self._lib.snn_seq_pack, n, C.byref(a), C.byref(b))
+
+    def unpack(self, q: Packed, x):
+        n = x.shape[-1]
+        a, b = self._seq(x, "x", n), self._seq(q, "q", n, packed=True)
+        self._call(self._lib.snn_seq_unpack, n, C.byref(b), C.byref(a))
+
+    # ---------------------------------------------------------------- convolution
+
+    def _conv_state(self, t, like, name):
+        return self._vec(t, like.dtype, self.batch * (self.taps - 1) * self.channels, name)
+
+    def conv_forward(self, x, w, bias, y, lengths=None, state=None, state_out=None, silu: bool = True):
+        """y = act(bias + taps of x); w [channels][taps].  state, state_out
+        [batch][taps - 1][channels]: the inputs before the first step and the
+        last ones."""
+        n = self.channels
+        a = snn_seq_conv(self._seq(x, "x", n), self._seq(y, "y", n), self._f32(w, n * self.taps, "w", True),
+                         self._f32(bias, n, "bias"), self._lengths(lengths), self._conv_state(state, x, "state"),
+                         self._conv_state(state_out, x, "state_out"), int(bool(silu)))
+        self._call(self._lib.snn_seq_conv_forward, C.byref(a))
+
+    def conv_backward(self, x, w, bias, dy, dx, dw, dbias=None, lengths=None, state=None, dstate_out=None,
+                      dstate=None, silu: bool = True):
+        """Gradients of conv_forward's inputs from dy (and dstate_out); x may
+        be Packed."""
+        n = self.channels
+        a = snn_seq_conv_grad(self._seq(x, "x", n, packed=True), self._seq(dy, "dy", n), self._seq(dx, "dx", n),
+                              self._f32(w, n * self.taps, "w", True), self._f32(bias, n, "bias"),
+                              self._f32(dw, n * self.taps, "dw", True), self._f32(dbias, n, "dbias"),
+                              self._lengths(lengths), self._conv_state(state, dy, "state"),
+                              self._conv_state(dstate_out, dy, "dstate_out"), self._conv_state(dstate, dy, "dstate"),
+                              int(bool(silu)))
+        self._call(self._lib.snn_seq_conv_backward, C.byref(a))
+
+    def conv_step(self, x, w, bias, state, state_out, y, silu: bool = True):
+        """One step of every sample: x, y [batch][channels]; state_out may be
+        state."""
+        n = self.channels
+        a = snn_seq_conv(self._seq(x, "x", n, rows=0), self._seq(y, "y", n, rows=0),
+                         self._f32(w, n * self.taps, "w", True), self._f32(bias, n, "bias"), None,
+                         self._conv_state(state, x, "state"), self._conv_state(state_out, x, "state_out"),
+                         int(bool(silu)))
+        self._call(self._lib.snn_seq_conv_step, C.byref(a))
+
+    # ---------------------------------------------------------------- scan
+
+    def _saved(self, saved):
+        if saved is None:
+            return None
+        return self._f32(saved, self.saved_shape[0] * self.saved_shape[1] * self.saved_shape[2] * self.saved_shape[3],
+                         "saved")
+
+    def _state(self, t, name, need=False):
+        return self._f32(t, self.batch * self.channels * self.state, name, need)
+
+    def scan_forward(self, u, delta, A, B, C_, y, D=None, z=None, delta_bias=None, h0=None, hT=None, saved=None,
+                     lengths=None, softplus: bool = True):
+        """y of the scan; B, C_ [batch][T][groups * state], A [channels][state],
+        h0, hT [batch][channels][state].  saved (shape ``saved_shape``, fp32)
+        is what scan_backward needs."""
+        n, gn = self.channels, self.groups * self.state
+        a = snn_seq_scan(self._seq(u, "u", n), self._seq(delta, "delta", n), self._seq(B, "B", gn),
+                         self._seq(C_, "C", gn), self._seq(z, "z", n, need=False), self._seq(y, "y", n),
+                         self._f32(A, n * self.state, "A", True), self._f32(D, n, "D"),
+                         self._f32(delta_bias, n, "delta_bias"), self._state(h0, "h0"), self._state(hT, "hT"),
+                         self._saved(saved), self._lengths(lengths), int(bool(softplus)))
+        self._call(self._lib.snn_seq_scan_forward, C.byref(a))
+
+    def scan_backward(self, u, delta, A, B, C_, dy, saved, du, ddelta, dA, dB, dC, D=None, z=None, delta_bias=None,
+                      dD=None, dz=None, ddelta_bias=None, h0=None, dhT=None, dh0=None, lengths=None,
+                      softplus: bool = True):
+        """Gradients of scan_forward's inputs from dy (and dhT); u, delta and z
+        may each be Packed.  saved None: the states are computed again from u,
+        delta, B and h0 (a layer made with ``recompute``), as belongs to packed
+        u and delta."""
+        n, gn = self.channels, self.groups * self.state
+        a = snn_seq_scan_grad(self._seq(u, "u", n, packed=True), self._seq(delta, "delta", n, packed=True),
+                              self._seq(B, "B", gn), self._seq(C_, "C", gn),
+                              self._seq(z, "z", n, packed=True, need=False), self._seq(dy, "dy", n),
+                              self._seq(du, "du", n), self._seq(ddelta, "ddelta", n), self._seq(dB, "dB", gn),
+                              self._seq(dC, "dC", gn), self._seq(dz, "dz", n, need=False),
+                              self._f32(A, n * self.state, "A", True), self._f32(D, n, "D"),
+                              self._f32(delta_bias, n, "delta_bias"), self._state(h0, "h0"), self._state(dhT, "dhT"),
+                              self._saved(saved),
+                              self._f32(dA, n * self.state, "dA", True), self._f32(dD, n, "dD"),
+                              self._f32(ddelta_bias, n, "ddelta_bias"), self._state(dh0, "dh0"),
+                              self._lengths(lengths), int(bool(softplus)))
+        self._call(self._lib.snn_seq_scan_backward, C.byref(a))
+
+    def scan_step(self, u, delta, A, B, C_, h, h_out, y, D=None, z=None, delta_bias=None, softplus: bool = True):
+        """One step of every sample: u, delta, z, y [batch][channels], B, C_
+        [batch][groups * state]; h_out may be h (None: zero)."""
+        n, gn = self.channels, self.groups * self.state
+        a = snn_seq_scan(self._seq(u, "u", n, rows=0), self._seq(delta, "delta", n, rows=0),
+                         self._seq(B, "B", gn, rows=0), self._seq(C_, "C", gn, rows=0),
+                         self._seq(z, "z", n, rows=0, need=False), self._seq(y, "y", n, rows=0),
+                         self._f32(A, n * self.state, "A", True), self._f32(D, n, "D"),
+                         self._f32(delta_bias, n, "delta_bias"), self._state(h, "h"),
+                         self._state(h_out, "h_out", True), None, None, int(bool(softplus)))
+        self._call(self._lib.snn_seq_scan_step, C.byref(a))
+
+
+class Sampler(_Handle):
+    """One snn_sampler handle: draws from up to `rows` rows of up to `n`
+    scores, bound to the current torch stream at creation."""
+
+    def __init__(self, rows: int, n: int, stream=None):
+        import torch
+        self._lib = _bind(load_library())
+        self._destroy, self._error = self._lib.snn_sampler_destroy, self._lib.snn_sampler_last_error
+        self.rows, self.n = int(rows), int(n)
+        self._open(stream)
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = self._lib.snn_sampler_create(self.rows, self.n, C.c_void_p(self.stream.cuda_stream), C.byref(h))
+        if rc != SNN_OK:
+            raise SNNError(rc, f"snn_sampler_create failed ({self._lib.snn_sampler_last_error(None).decode()})")
+        self._h = h
+
+    def sample(self, scores, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None):
+        """token [rows] (int32): a class for each row of scores [rows][n] by
+        the random numbers u [rows] in [0, 1).  temperature, top_p, min_p
+        (fp32), top_k (int32) hold a value for each row, or None: 1, all, 0,
+        all.  logprob [rows]: the drawn classes' log-probabilities among
+        those that the filters keep."""
+        import torch
+        if scores.dim() != 2 or (scores.stride(1) != 1 and scores.shape[1] > 1):
+            raise ValueError("scores must be [rows][n] with a contiguous last dimension")
+        self._on_device(scores, "scores")
+        R, n = scores.shape
+        a = snn_sample_args(scores.data_ptr(), scores.stride(0), _dtype(scores), R, n, self._f32(u, R, "u", True),
+                            self._f32(temperature, R, "temperature"), self._vec(top_k, torch.int32, R, "top_k"),
+                            self._f32(top_p, R, "top_p"), self._f32(min_p, R, "min_p"),
+                            self._vec(token, torch.int32, R, "token", True), self._f32(logprob, R, "logprob"))
+        self._call(self._lib.snn_sampler_sample, C.byref(a))
