@@ -30,13 +30,13 @@ __device__ __forceinline__ void conv_in(const ConvArgs& a, int b, int t, int len
     if (t >= 0) {
         Raw<T, VW, PK> r;
         raw_load(r, a.x, b, t, a.T, c, t < len ? n : 0);
-        raw_get(r, a.x, o);
+        raw_get(r, a.x, c, o);
         return;
     }
     const SeqT s{const_cast<char*>(a.state), nullptr, a.channels, (long long)(a.taps - 1) * a.channels, 0, 0};
     Raw<T, VW, false> r;
     raw_load(r, s, b, a.taps - 1 + t, a.T, c, a.state ? n : 0);
-    raw_get(r, s, o);
+    raw_get(r, s, c, o);
 }
 
 template <class T, int K>
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kConvLanes * kConvRows) conv_backward_kernel(C
             float dy[VW];
             Raw<T, VW, false> r;
             raw_load(r, a.dy, b, t, a.T, c, t < len ? n : 0);
-            raw_get(r, a.dy, dy);
+            raw_get(r, a.dy, c, dy);
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
                 float d = dy[i];

@@ -21,7 +21,7 @@ struct Vec<T, 1> {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float sigmoid(float x) {
     return rcp_fast(1.0f + exp2_fast(-kLog2e * x));
@@ -52,13 +52,13 @@ __device__ __forceinline__ float softplus(float x, float& sig) {
 // that straddle two blocks have two scales.
 template <class T, int N, bool PK>
 struct Raw {
+    static constexpr int BYTES = N * sizeof(T), WORDS = (BYTES + 3) / 4;
     union {
         typename Vec<T, N>::type v;
         T e[N];
-        unsigned char b[N * sizeof(T)];
+        unsigned w[WORDS];     // packed: byte i in word i / 4
     };
     float scale[PK ? 2 : 1];
-    int split;                 // the first value of the second block
 };
 
 template <class T, int N, bool PK>
@@ -68,23 +68,19 @@ __device__ __forceinline__ void raw_load(Raw<T, N, PK>& r, const SeqT& s, long l
         if (s.packed) {
             const long long at = (b * T_ + t) * s.row + c;
             const unsigned char* p = reinterpret_cast<const unsigned char*>(s.p) + at;
+            unsigned w[(N + 3) / 4] = {};
             if (n >= N) {
-                typedef typename Vec<unsigned char, N>::type V;
-                const V v = *reinterpret_cast<const V*>(p);
-                if constexpr (N == 1) r.b[0] = v;
-                else {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) r.b[i] = v[i];
-                }
+                __builtin_memcpy(w, p, N);
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) r.b[i] = i < n ? p[i] : 0;
+                for (int i = 0; i < N; ++i) w[i / 4] |= (i < n ? (unsigned)p[i] : 0u) << (8 * (i % 4));
             }
+#pragma unroll
+            for (int i = 0; i < (N + 3) / 4; ++i) r.w[i] = w[i];
             const float* sc = s.scale + (b * T_ + t) * s.blocks;
-            const int k = c / SNN_SEQ_BLOCK;
-            r.split = (k + 1) * SNN_SEQ_BLOCK - c;
+            const int k = c / SNN_SEQ_BLOCK, split = (k + 1) * SNN_SEQ_BLOCK - c;
             r.scale[0] = n > 0 ? sc[k] : 0.0f;
-            r.scale[1] = r.split < min(n, N) ? sc[k + 1] : r.scale[0];
+            r.scale[1] = split < min(n, N) ? sc[k + 1] : r.scale[0];
             return;
         }
     }
@@ -98,12 +94,19 @@ __device__ __forceinline__ void raw_load(Raw<T, N, PK>& r, const SeqT& s, long l
 }
 
 template <class T, int N, bool PK>
-__device__ __forceinline__ void raw_get(const Raw<T, N, PK>& r, const SeqT& s, float (&o)[N]) {
+__device__ __forceinline__ void raw_get(const Raw<T, N, PK>& r, const SeqT& s, int c, float (&o)[N]) {
     if constexpr (PK) {
         if (s.packed) {
+            const int split = (c / SNN_SEQ_BLOCK + 1) * SNN_SEQ_BLOCK - c;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                o[i] = __builtin_amdgcn_cvt_f32_fp8((int)r.b[i], 0) * (i < r.split ? r.scale[0] : r.scale[1]);
+            for (int i = 0; i < N; ++i) {
+                const int w = (int)r.w[i / 4];
+                const float x = i % 4 == 0   ? __builtin_amdgcn_cvt_f32_fp8(w, 0)
+                                : i % 4 == 1 ? __builtin_amdgcn_cvt_f32_fp8(w, 1)
+                                : i % 4 == 2 ? __builtin_amdgcn_cvt_f32_fp8(w, 2)
+                                             : __builtin_amdgcn_cvt_f32_fp8(w, 3);
+                o[i] = x * (i < split ? r.scale[0] : r.scale[1]);
+            }
             return;
         }
     }

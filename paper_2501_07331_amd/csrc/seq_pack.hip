@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
     Raw<T, 8, false> r;
     float x[8], m = 0.0f;
     raw_load(r, a.x, bt / a.T, bt % a.T, a.T, c, n);
-    raw_get(r, a.x, x);
+    raw_get(r, a.x, c, x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float v = fabsf(x[j]);
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256) unpack_kernel(PackArgs a) {
     Raw<T, 8, true> r;
     float x[8];
     raw_load(r, q, bt / a.T, bt % a.T, a.T, c, a.n - c);
-    raw_get(r, q, x);
+    raw_get(r, q, c, x);
     store_vec<T, 8>(a.x, bt / a.T, bt % a.T, c, a.n - c, x);
 }
 

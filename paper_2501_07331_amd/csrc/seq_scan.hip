@@ -96,6 +96,8 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
         h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
     }
 
+    constexpr int R = S < 4 ? S : 4;
+    float ykeep = 0.0f;
     Raw<T, VW, STATES> ru[NV], rd[NV], rz[NV];   // only a backward pass has packed inputs
     GroupTile<T, S, TT, STATES> gt;
     auto load = [&](int t0) {
@@ -119,9 +121,9 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
             const int r = erow + v * PR;
             const bool in = t0 + r < len && t0 + r < t_end;
             float d[VW], z[VW];
-            raw_get(ru[v], a.u, u[v]);
-            raw_get(rd[v], a.delta, d);
-            if (!STATES && a.z.p) raw_get(rz[v], a.z, z);
+            raw_get(ru[v], a.u, c0 + ecol, u[v]);
+            raw_get(rd[v], a.delta, c0 + ecol, d);
+            if (!STATES && a.z.p) raw_get(rz[v], a.z, c0 + ecol, z);
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
                 float sig;
@@ -163,8 +165,10 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
                     y = fmaf(Cv.z, h[2], y);
                     y = fmaf(Cv.w, h[3], y);
                     y = lanes_sum<S>(y);
-                    // this channel's lanes, all of one wave, have read the pair
-                    if (q == 0) ds[r][ch].x = y;
+                    // the sum is in all of the channel's lanes: each keeps one of R steps, for one store
+                    ykeep = j % R == 0 || q == j % R ? y : ykeep;
+                    // the channel's lanes, all of one wave, have read these steps' pairs
+                    if (j % R == R - 1 && (S <= R || q < R)) ds[r - (R - 1) + q][ch].x = ykeep;
                 }
             }
         }

@@ -15,6 +15,8 @@
 
 namespace {
 
+constexpr int kAhead = 4;
+
 template <int S>
 struct BwdShape {
     static constexpr int NP = 4 * S;
@@ -45,18 +47,26 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // One part of the time axis of CB channels.  STATES: only the adjoint at the
 // part's start from zero at its end, and the sum of its delta'.
-template <class T, int S, bool STATES>
-__global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs a) {
+//
+// The states of a segment and their decays take 132 registers a lane; what
+// the elementwise work needs before and after them waits in LDS, so that two
+// waves fit on a SIMD.
+template <class T, int S, bool STATES, bool PK>
+__global__ void __launch_bounds__(BwdShape<S>::NT) __attribute__((amdgpu_waves_per_eu(S == 1 ? 1 : 2, S == 1 ? 1 : 2)))
+scan_backward_kernel(ScanArgs a) {
     constexpr int NP = BwdShape<S>::NP, CB = BwdShape<S>::CB, NT = BwdShape<S>::NT, TT = kScanSeg;
     constexpr int W = BwdShape<S>::WAVES;
     constexpr int EP = TT * CB / NT;
     constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
     constexpr int BW = 2 * NP, BE = (TT * BW + NT - 1) / NT;
-    __shared__ float2 ds[TT][CB];                  // (delta', delta' u), then (s1, s2)
+    constexpr int TK = STATES ? 1 : TT;
+    __shared__ float2 ds[TT][CB];                  // (delta', delta' u), then (s1, s2 / ln 2)
     __shared__ float dyl[TT][CB];                  // dy'
-    __shared__ float yl[STATES ? 1 : TT][CB];      // sum_n C h
+    __shared__ float yl[TK][CB];                   // sum_n C h
+    __shared__ __align__(16) float ul[TK][CB], dl[TK][CB], sl[TK][CB], wl[TK][CB];   // u, delta', its slope, dy silu'(z)
+    __shared__ float pl[2][CB];                    // delta_bias, D
     __shared__ __align__(16) float bc[TT * BW];
-    __shared__ float red[STATES ? 1 : TT][W][BW];  // the waves' shares of dB, dC
+    __shared__ float red[TK][W][BW];               // the waves' shares of dB, dC
 
     const int tid = threadIdx.x;
     const int nblk = a.groups * a.gblocks;
@@ -67,23 +77,22 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
     const int t_begin = part * a.chunk_len, t_end = min(a.T, t_begin + a.chunk_len);
 
     const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
-    float bias[VW], Dv[VW], sumD[VW], sumB[VW];
+    float sumD[VW], sumB[VW];
 #pragma unroll
-    for (int i = 0; i < VW; ++i) {
-        bias[i] = a.delta_bias && i < en ? a.delta_bias[c0 + ecol + i] : 0.0f;
-        Dv[i] = a.D && i < en ? a.D[c0 + ecol + i] : 0.0f;
-        sumD[i] = sumB[i] = 0.0f;
+    for (int i = 0; i < VW; ++i) sumD[i] = sumB[i] = 0.0f;
+    for (int i = tid; i < CB; i += NT) {
+        pl[0][i] = a.delta_bias && i < nc ? a.delta_bias[c0 + i] : 0.0f;
+        pl[1][i] = a.D && i < nc ? a.D[c0 + i] : 0.0f;
     }
     const int ch = tid / S, q = tid % S, wave = tid / 64, lane = tid % 64;
     const bool live = ch < nc;
     const long long cidx = (long long)b * a.channels + c0 + ch;
-    float A[4], A2[4], gr[4], dA[4], dsum = 0.0f;
+    float A2[4], gr[4], dA[4], dsum = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int n = 4 * q + k;
         const bool in = live && n < a.state;
-        A[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] : 0.0f;
-        A2[k] = A[k] * kLog2e;
+        A2[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] * kLog2e : 0.0f;
         dA[k] = gr[k] = 0.0f;
         if (!STATES && a.chunks == 1 && in && a.dhT) gr[k] = a.dhT[cidx * a.state + n];
     }
@@ -93,7 +102,44 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
         gr[0] = v.x, gr[1] = v.y, gr[2] = v.z, gr[3] = v.w;
     }
 
+    constexpr int R = S < 4 ? S : 4, M = 16 / S < 4 ? 16 / S : 4;
+    const int copy = lane % 16 / S;
+    const int at = (lane >> 5) * NP + 4 * q + 2 * ((lane >> 4) & 1);
+    float k0 = 0.0f, k1 = 0.0f, m0 = 0.0f, m1 = 0.0f;
+
+    // a tile's inputs as they lie in memory, loaded while the one behind it is worked on
+    Raw<T, VW, PK> ru[NV], rd[NV], rz[NV];
+    Raw<T, VW, false> ry[NV];
+    T rb[BE];
+    float4 h4;
+    auto load = [&](int t0) {
+        h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (t0 >= len) return;
+        if (!STATES && live)
+            h4 = *reinterpret_cast<const float4*>(
+                a.saved + (((long long)b * a.segs + t0 / TT) * a.channels + c0 + ch) * NP + 4 * q);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int t = t0 + erow + v * PR, n = t < len && t < t_end ? en : 0;
+            raw_load(ru[v], a.u, b, t, a.T, c0 + ecol, n);
+            raw_load(rd[v], a.delta, b, t, a.T, c0 + ecol, n);
+            raw_load(ry[v], a.dy, b, t, a.T, c0 + ecol, n);
+            if (a.z.p) raw_load(rz[v], a.z, b, t, a.T, c0 + ecol, n);
+        }
+#pragma unroll
+        for (int e = 0; e < BE; ++e) {
+            const int i = e * NT + tid, t = t0 + i / BW, k = i % BW, n = k % NP;
+            rb[e] = T(0.0f);
+            if (i < TT * BW && t < len && t < t_end && n < a.state) {
+                const SeqT& s = k < NP ? a.B : a.C;
+                rb[e] = reinterpret_cast<const T*>(s.p)[b * s.sample + t * s.row + (long long)g * a.state + n];
+            }
+        }
+    };
+
     const int last = t_begin + (t_end - 1 - t_begin) / TT * TT;
+    load(last);
+    __syncthreads();                               // pl
     for (int t0 = last; t0 >= t_begin; t0 -= TT) {
         if (t0 >= len) {
             // nothing of the sample: the outputs' rows are zero
@@ -108,56 +154,44 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
                     if (a.dz.p) store_vec<T, VW>(a.dz, b, t, c0 + ecol, en, zero);
                 }
             }
+            if (t0 > t_begin) load(t0 - TT);
             continue;
-        }
-        float4 h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (!STATES && live)
-            h4 = *reinterpret_cast<const float4*>(
-                a.saved + (((long long)b * a.segs + t0 / TT) * a.channels + c0 + ch) * NP + 4 * q);
-        float u[NV][VW], d[NV][VW], sg[NV][VW], dy[NV][VW], z[NV][VW];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int t = t0 + erow + v * PR, n = t < len && t < t_end ? en : 0;
-            Raw<T, VW, true> r;
-            Raw<T, VW, false> rp;
-            raw_load(r, a.u, b, t, a.T, c0 + ecol, n);
-            raw_get(r, a.u, u[v]);
-            raw_load(r, a.delta, b, t, a.T, c0 + ecol, n);
-            raw_get(r, a.delta, d[v]);
-            raw_load(rp, a.dy, b, t, a.T, c0 + ecol, n);
-            raw_get(rp, a.dy, dy[v]);
-            if (a.z.p) {
-                raw_load(r, a.z, b, t, a.T, c0 + ecol, n);
-                raw_get(r, a.z, z[v]);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < BE; ++e) {
-            const int i = e * NT + tid, t = t0 + i / BW, k = i % BW, n = k % NP;
-            float x = 0.0f;
-            if (i < TT * BW && t < len && t < t_end && n < a.state) {
-                const SeqT& s = k < NP ? a.B : a.C;
-                x = (float)reinterpret_cast<const T*>(s.p)[b * s.sample + t * s.row + (long long)g * a.state + n];
-            }
-            if (i < TT * BW) bc[i] = x;
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int r = erow + v * PR;
             const bool in = t0 + r < len && t0 + r < t_end;
+            float u[VW], d[VW], dy[VW], z[VW];
+            raw_get(ru[v], a.u, c0 + ecol, u);
+            raw_get(rd[v], a.delta, c0 + ecol, d);
+            raw_get(ry[v], a.dy, c0 + ecol, dy);
+            if (a.z.p) raw_get(rz[v], a.z, c0 + ecol, z);
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
-                float x = d[v][i] + bias[i], sig = 1.0f;
+                float x = d[i] + pl[0][ecol + i], sig = 1.0f;
                 if (a.softplus) x = softplus(x, sig);
                 x = in && i < en ? x : 0.0f;
-                d[v][i] = x;
-                sg[v][i] = sig;
-                ds[r][ecol + i] = make_float2(x, x * u[v][i]);
-                const float gate = a.z.p ? z[v][i] * sigmoid(z[v][i]) : 1.0f;
-                dyl[r][ecol + i] = dy[v][i] * gate;
+                ds[r][ecol + i] = make_float2(x, x * u[i]);
+                float gate = 1.0f;
+                if (a.z.p) {
+                    const float p = sigmoid(z[i]);
+                    gate = z[i] * p;
+                    if (!STATES) wl[r][ecol + i] = dy[i] * (p * fmaf(z[i], 1.0f - p, 1.0f));
+                }
+                dyl[r][ecol + i] = dy[i] * gate;
+                if constexpr (!STATES) {
+                    ul[r][ecol + i] = u[i];
+                    dl[r][ecol + i] = x;
+                    sl[r][ecol + i] = in ? sig : 0.0f;
+                }
             }
         }
+#pragma unroll
+        for (int e = 0; e < BE; ++e)
+            if (e * NT + tid < TT * BW) bc[e * NT + tid] = (float)rb[e];
+        const float4 hs = h4;
         __syncthreads();
+        if (t0 > t_begin) load(t0 - TT);
 
         if constexpr (STATES) {
 #pragma unroll
@@ -174,7 +208,7 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
         } else {
             // the states before each step, and the decays
             float h[TT + 1][4], dec[TT][4];
-            h[0][0] = h4.x, h[0][1] = h4.y, h[0][2] = h4.z, h[0][3] = h4.w;
+            h[0][0] = hs.x, h[0][1] = hs.y, h[0][2] = hs.z, h[0][3] = hs.w;
 #pragma unroll
             for (int r = 0; r < TT; ++r) {
                 const float2 x = ds[r][ch];
@@ -185,16 +219,21 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
                     dec[r][k] = exp2_fast(x.x * A2[k]);
                     h[r + 1][k] = fmaf(dec[r][k], h[r][k], x.y * Bk[k]);
                 }
-                if (a.z.p) {
-                    const float4 Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
-                    float y = Cv.x * h[r + 1][0];
-                    y = fmaf(Cv.y, h[r + 1][1], y);
-                    y = fmaf(Cv.z, h[r + 1][2], y);
-                    y = fmaf(Cv.w, h[r + 1][3], y);
-                    y = lanes_sum<S>(y);
-                    if (q == 0) yl[r][ch] = y;
-                }
+                // the gate's gradient needs it; without a gate a branch here would cost more
+                const float4 Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
+                float y = Cv.x * h[r + 1][0];
+                y = fmaf(Cv.y, h[r + 1][1], y);
+                y = fmaf(Cv.z, h[r + 1][2], y);
+                y = fmaf(Cv.w, h[r + 1][3], y);
+                y = lanes_sum<S>(y);
+                // each of the channel's lanes keeps one of R steps, for one store
+                k0 = r % R == 0 || q == r % R ? y : k0;
+                if (r % R == R - 1 && (S <= R || q < R)) yl[r - (R - 1) + q][ch] = k0;
+                // reads of LDS run ahead of their use by at most kAhead steps, for the registers' sake
+                if (r % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
             }
+            // B and delta' are read again: kept from above they would fill the registers
+            asm volatile("" ::: "memory");
 #pragma unroll
             for (int r = TT - 1; r >= 0; --r) {
                 const float2 x = ds[r][ch];
@@ -208,15 +247,17 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
                     gr[k] = fmaf(Ck[k], dyp, gr[k]);
                     dB[k] = gr[k] * x.y;
                     dC[k] = dyp * h[r + 1][k];
-                    s1 = fmaf(gr[k], Bk[k], s1);
+                    s1 = k ? fmaf(gr[k], Bk[k], s1) : gr[k] * Bk[k];
                     gr[k] *= dec[r][k];
                     const float p = gr[k] * h[r][k];
-                    s2 = fmaf(p, A[k], s2);
+                    s2 = k ? fmaf(p, A2[k], s2) : p * A2[k];
                     dA[k] = fmaf(p, x.x, dA[k]);
                 }
                 s1 = lanes_sum<S>(s1);
                 s2 = lanes_sum<S>(s2);
-                if (q == 0) ds[r][ch] = make_float2(s1, s2);
+                k0 = r % R == R - 1 || q == r % R ? s1 : k0;
+                k1 = r % R == R - 1 || q == r % R ? s2 : k1;
+                if (r % R == 0 && (S <= R || q < R)) ds[r + q][ch] = make_float2(k0, k1);
                 // rows of 16 lanes 0, 1: dB of states 0 1, 2 3 of the lane's four; rows 2, 3: dC
 #pragma unroll
                 for (int k = 0; k < 4; ++k) swap_add32(dB[k], dC[k]);
@@ -224,10 +265,12 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
                 swap_add16(dB[1], dB[3]);
                 dB[0] = row_sum<S>(dB[0]);
                 dB[1] = row_sum<S>(dB[1]);
-                if (lane % 16 < S) {
-                    const int at = (lane >> 5) * NP + 4 * q + 2 * ((lane >> 4) & 1);
-                    *reinterpret_cast<float2*>(&red[r][wave][at]) = make_float2(dB[0], dB[1]);
-                }
+                // the sums are in 16 / S lanes of each row: each keeps one of M steps
+                m0 = r % M == M - 1 || copy == r % M ? dB[0] : m0;
+                m1 = r % M == M - 1 || copy == r % M ? dB[1] : m1;
+                if (r % M == 0 && (16 / S <= M || copy < M))
+                    *reinterpret_cast<float2*>(&red[r + copy][wave][at]) = make_float2(m0, m1);
+                if (r % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
             }
         }
         __syncthreads();
@@ -239,18 +282,14 @@ __global__ void __launch_bounds__(BwdShape<S>::NT) scan_backward_kernel(ScanArgs
                 float du[VW], dd[VW], dz[VW];
 #pragma unroll
                 for (int i = 0; i < VW; ++i) {
+                    const int c = ecol + i;
                     const bool in = t < len && i < en;
-                    const float2 s = ds[r][ecol + i];
-                    float dyp = dy[v][i];
-                    dz[i] = 0.0f;
-                    if (a.z.p) {
-                        const float p = sigmoid(z[v][i]), y = fmaf(Dv[i], u[v][i], yl[r][ecol + i]);
-                        dz[i] = in ? dy[v][i] * y * (p * fmaf(z[v][i], 1.0f - p, 1.0f)) : 0.0f;
-                        dyp *= z[v][i] * p;
-                    }
-                    du[i] = in ? fmaf(Dv[i], dyp, d[v][i] * s.x) : 0.0f;
-                    dd[i] = in ? fmaf(u[v][i], s.x, s.y) * sg[v][i] : 0.0f;
-                    sumD[i] = in ? fmaf(dyp, u[v][i], sumD[i]) : sumD[i];
+                    const float2 s = ds[r][c];
+                    const float u = ul[r][c], dyp = dyl[r][c], D = pl[1][c];
+                    dz[i] = in && a.z.p ? wl[r][c] * fmaf(D, u, yl[r][c]) : 0.0f;
+                    du[i] = in ? fmaf(D, dyp, dl[r][c] * s.x) : 0.0f;
+                    dd[i] = in ? fmaf(u, s.x, s.y * kLn2) * sl[r][c] : 0.0f;
+                    sumD[i] = in ? fmaf(dyp, u, sumD[i]) : sumD[i];
                     sumB[i] += dd[i];
                 }
                 store_vec<T, VW>(a.du, b, t, c0 + ecol, en, du);
@@ -365,22 +404,27 @@ __global__ void __launch_bounds__(256) scan_sums_kernel(ScanArgs a, int NP, int 
     }
 }
 
-template <class T, int S>
-hipError_t backward(const ScanArgs& a, hipStream_t s) {
+template <class T, int S, bool PK>
+hipError_t passes(const ScanArgs& a, hipStream_t s) {
     constexpr int NP = BwdShape<S>::NP;
     const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(BwdShape<S>::NT);
     if (a.chunks > 1) {
         // the first part's start is nobody's end
-        scan_backward_kernel<T, S, true><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
+        scan_backward_kernel<T, S, true, PK><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
         const long long n = (long long)a.batch * a.channels * NP;
         scan_join_back_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, NP);
     }
-    scan_backward_kernel<T, S, false><<<grid, block, 0, s>>>(a);
+    scan_backward_kernel<T, S, false, PK><<<grid, block, 0, s>>>(a);
     const long long bc = (long long)a.batch * a.T * 2 * a.groups * a.state;
     const long long cols = (long long)a.channels * (NP + 2);
     const int bc_blocks = (int)((bc + 255) / 256);
     scan_sums_kernel<T><<<(unsigned)(bc_blocks + (cols + 31) / 32), 256, 0, s>>>(a, NP, bc_blocks);
     return hipGetLastError();
+}
+
+template <class T, int S>
+hipError_t backward(const ScanArgs& a, hipStream_t s) {
+    return a.u.packed || a.delta.packed || a.z.packed ? passes<T, S, true>(a, s) : passes<T, S, false>(a, s);
 }
 
 }  // namespace
