@@ -27,24 +27,19 @@ __device__ __forceinline__ float sigmoid(float x) {
     return rcp_fast(1.0f + exp2_fast(-kLog2e * x));
 }
 
-// softplus(x) = max(x, 0) + log(1 + e) with e = exp(-|x|), and
-// log(1 + e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by the artanh series:
-// relative error below 1e-7 down to the smallest results, where log(1 + e)
-// itself would lose the low bits of e.  sig: its derivative, sigmoid(x).
+// softplus(x) = max(x, 0) + log(1 + e) with e = exp(-|x|).  With w the
+// rounded 1 + e, log(1 + e) = log(w) e / (w - 1) to the last bits (Kahan's
+// form: what rounding w takes from e it takes from w - 1 too), so that the
+// smallest results keep their relative precision: below 7e-7 down to e^-9,
+// 1.8e-6 down to e^-30, where exp's own argument is what is left of it.
+// sig: its derivative, sigmoid(x).
 __device__ __forceinline__ float softplus(float x, float& sig) {
     const float e = exp2_fast(-kLog2e * fabsf(x));
-    const float r = rcp_fast(1.0f + e);
+    const float w = 1.0f + e, d = w - 1.0f;
+    const float r = rcp_fast(w);
     sig = x >= 0.0f ? r : e * r;
-    const float s = e * rcp_fast(2.0f + e);
-    const float q = s * s;
-    float p = fmaf(q, 1.0f / 15.0f, 1.0f / 13.0f);
-    p = fmaf(p, q, 1.0f / 11.0f);
-    p = fmaf(p, q, 1.0f / 9.0f);
-    p = fmaf(p, q, 1.0f / 7.0f);
-    p = fmaf(p, q, 1.0f / 5.0f);
-    p = fmaf(p, q, 1.0f / 3.0f);
-    p = fmaf(p, q, 1.0f);
-    return fmaf(s + s, p, fmaxf(x, 0.0f));
+    const float p = d > 0.0f ? __builtin_amdgcn_logf(w) * kLn2 * (e * rcp_fast(d)) : e;
+    return __builtin_amdgcn_fmed3f(x, 0.0f, INFINITY) + p;    // NaN: p is NaN
 }
 
 // N values of a row as they lie in memory, and as fp32.  n: how many of them
@@ -62,35 +57,40 @@ struct Raw {
 };
 
 template <class T, int N, bool PK>
-__device__ __forceinline__ void raw_load(Raw<T, N, PK>& r, const SeqT& s, long long b, long long t, int T_, int c,
-                                         int n) {
-    if constexpr (PK) {
-        if (s.packed) {
-            const long long at = (b * T_ + t) * s.row + c;
-            const unsigned char* p = reinterpret_cast<const unsigned char*>(s.p) + at;
-            unsigned w[(N + 3) / 4] = {};
-            if (n >= N) {
-                __builtin_memcpy(w, p, N);
-            } else {
+__device__ __forceinline__ void raw_packed(Raw<T, N, PK>& r, const unsigned char* p, const float* sc, int c, int n) {
+    unsigned w[(N + 3) / 4] = {};
+    if (n >= N) {
+        __builtin_memcpy(w, p, N);
+    } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) w[i / 4] |= (i < n ? (unsigned)p[i] : 0u) << (8 * (i % 4));
-            }
-#pragma unroll
-            for (int i = 0; i < (N + 3) / 4; ++i) r.w[i] = w[i];
-            const float* sc = s.scale + (b * T_ + t) * s.blocks;
-            const int k = c / SNN_SEQ_BLOCK, split = (k + 1) * SNN_SEQ_BLOCK - c;
-            r.scale[0] = n > 0 ? sc[k] : 0.0f;
-            r.scale[1] = split < min(n, N) ? sc[k + 1] : r.scale[0];
-            return;
-        }
+        for (int i = 0; i < N; ++i) w[i / 4] |= (i < n ? (unsigned)p[i] : 0u) << (8 * (i % 4));
     }
-    const T* p = reinterpret_cast<const T*>(s.p) + b * s.sample + t * s.row + c;
+#pragma unroll
+    for (int i = 0; i < (N + 3) / 4; ++i) r.w[i] = w[i];
+    const int split = (c / SNN_SEQ_BLOCK + 1) * SNN_SEQ_BLOCK - c;
+    r.scale[0] = n > 0 ? sc[0] : 0.0f;
+    r.scale[1] = split < min(n, N) ? sc[1] : r.scale[0];
+}
+template <class T, int N, bool PK>
+__device__ __forceinline__ void raw_dense(Raw<T, N, PK>& r, const T* p, int n) {
     if (n >= N) {
         r.v = *reinterpret_cast<const typename Vec<T, N>::type*>(p);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) r.e[i] = i < n ? p[i] : T(0.0f);
     }
+}
+template <class T, int N, bool PK>
+__device__ __forceinline__ void raw_load(Raw<T, N, PK>& r, const SeqT& s, long long b, long long t, int T_, int c,
+                                         int n) {
+    if constexpr (PK) {
+        if (s.packed) {
+            raw_packed(r, reinterpret_cast<const unsigned char*>(s.p) + (b * T_ + t) * s.row + c,
+                       s.scale + (b * T_ + t) * s.blocks + c / SNN_SEQ_BLOCK, c, n);
+            return;
+        }
+    }
+    raw_dense(r, reinterpret_cast<const T*>(s.p) + b * s.sample + t * s.row + c, n);
 }
 
 template <class T, int N, bool PK>
@@ -115,8 +115,7 @@ __device__ __forceinline__ void raw_get(const Raw<T, N, PK>& r, const SeqT& s, i
 }
 
 template <class T, int N>
-__device__ __forceinline__ void store_vec(const SeqT& s, long long b, long long t, int c, int n, const float (&o)[N]) {
-    T* p = reinterpret_cast<T*>(s.p) + b * s.sample + t * s.row + c;
+__device__ __forceinline__ void store_at(T* p, int n, const float (&o)[N]) {
     if (n >= N) {
         if constexpr (N == 1) *p = (T)o[0];
         else {
@@ -129,6 +128,77 @@ __device__ __forceinline__ void store_vec(const SeqT& s, long long b, long long 
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < n) p[i] = (T)o[i];
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_vec(const SeqT& s, long long b, long long t, int c, int n, const float (&o)[N]) {
+    store_at<T, N>(reinterpret_cast<T*>(s.p) + b * s.sample + t * s.row + c, n, o);
+}
+
+// N neighbouring values of a sequence's rows, read tile by tile: a thread's
+// address at its first row is made once, and a tile adds what is the same for
+// all threads.
+template <class T, int N, bool PK>
+struct RowIn {
+    const char* p;
+    const float* sc;
+    __device__ __forceinline__ void init(const SeqT& s, long long b, long long t, int T_, int c) {
+        sc = nullptr;
+        if (PK && s.packed) {
+            p = s.p + (b * T_ + t) * s.row + c;
+            sc = s.scale + (b * T_ + t) * s.blocks + c / SNN_SEQ_BLOCK;
+        } else {
+            p = s.p + (b * s.sample + t * s.row + c) * (long long)sizeof(T);
+        }
+    }
+    // t: rows past the first one
+    __device__ __forceinline__ void load(Raw<T, N, PK>& r, const SeqT& s, long long t, int c, int n) const {
+        if constexpr (PK) {
+            if (s.packed) {
+                raw_packed(r, reinterpret_cast<const unsigned char*>(p + t * s.row), sc + t * s.blocks, c, n);
+                return;
+            }
+        }
+        raw_dense(r, reinterpret_cast<const T*>(p + t * s.row * (long long)sizeof(T)), n);
+    }
+};
+template <class T, int N>
+struct RowOut {
+    char* p;
+    __device__ __forceinline__ void init(const SeqT& s, long long b, long long t, int c) {
+        p = s.p + (b * s.sample + t * s.row + c) * (long long)sizeof(T);
+    }
+    __device__ __forceinline__ void store(const SeqT& s, long long t, int n, const float (&o)[N]) const {
+        store_at<T, N>(reinterpret_cast<T*>(p + t * s.row * (long long)sizeof(T)), n, o);
+    }
+};
+
+// N consecutive floats of LDS.
+template <int N>
+__device__ __forceinline__ void lds_get(const float* p, float (&o)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + i);
+            o[i] = v.x, o[i + 1] = v.y, o[i + 2] = v.z, o[i + 3] = v.w;
+        }
+    } else if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2*>(p);
+        o[0] = v.x, o[1] = v.y;
+    } else {
+        o[0] = *p;
+    }
+}
+template <int N>
+__device__ __forceinline__ void lds_put(float* p, const float (&o)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            *reinterpret_cast<float4*>(p + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+    } else if constexpr (N == 2) {
+        *reinterpret_cast<float2*>(p) = make_float2(o[0], o[1]);
+    } else {
+        *p = o[0];
     }
 }
 

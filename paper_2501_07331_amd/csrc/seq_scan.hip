@@ -7,45 +7,9 @@
 // is elementwise in (step, channel) -- softplus, delta' u, the gate -- is done
 // once per element by all threads on 16-byte vectors before and after the
 // tile's steps, and passes through LDS.
-#include "seq_device.h"
+#include "seq_scan.h"
 
 namespace {
-
-template <int S>
-struct ScanShape {
-    static constexpr int NP = 4 * S;                            // states of a channel, padded
-    static constexpr int CB = S <= 4 ? 64 : S == 8 ? 32 : 16;   // channels of a workgroup
-    static constexpr int NT = CB * S;                           // threads
-};
-
-// Staging of B and C (one of them: ONE) of a tile: [TT][2][NP] fp32 in LDS,
-// zero past the sample's steps and the states.
-template <class T, int S, int TT, bool ONE>
-struct GroupTile {
-    static constexpr int NP = ScanShape<S>::NP, NT = ScanShape<S>::NT;
-    static constexpr int W = ONE ? NP : 2 * NP, E = (TT * W + NT - 1) / NT;
-    T raw[E];
-    __device__ __forceinline__ void load(const ScanArgs& a, const SeqT& first, const SeqT& second, int b, int g, int t0,
-                                         int len, int tid) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = e * NT + tid, t = t0 + i / W, k = i % W, n = k % NP;
-            raw[e] = T(0.0f);
-            if (i < TT * W && t < len && n < a.state) {
-                const SeqT& s = k < NP ? first : second;
-                raw[e] = reinterpret_cast<const T*>(s.p)[(long long)b * s.sample + (long long)t * s.row +
-                                                         (long long)g * a.state + n];
-            }
-        }
-    }
-    __device__ __forceinline__ void store(float* bc, int tid) const {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = e * NT + tid;
-            if (i < TT * W) bc[i] = (float)raw[e];
-        }
-    }
-};
 
 // What a launch is for: the whole scan; only the saved states (they are
 // computed again for the backward pass); only a part's last state from zero
@@ -59,7 +23,9 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
     constexpr bool STATES = MODE != SCAN_ALL, ENDS = MODE == SCAN_ENDS;
     constexpr int EP = TT * CB / NT;              // elements a thread
     constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
-    __shared__ float2 ds[TT][CB];                 // (delta', delta' u); y in its first half
+    __shared__ __align__(16) float2 ds[TT][CB];   // (delta', delta' u)
+    // sum_n C h; four steps are written at once, which the padding puts on different banks
+    __shared__ __align__(16) float yl[STATES ? 1 : TT][CB + 16];
     __shared__ __align__(16) float bc[TT * (STATES ? NP : 2 * NP)];
 
     const int tid = threadIdx.x;
@@ -71,6 +37,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
 
     // elementwise role: VW channels from ecol of the rows erow, erow + PR, ...
     const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
+    const bool gated = !STATES && a.z.p;
     float bias[VW], Dv[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
@@ -99,17 +66,24 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
     constexpr int R = S < 4 ? S : 4;
     float ykeep = 0.0f;
     Raw<T, VW, STATES> ru[NV], rd[NV], rz[NV];   // only a backward pass has packed inputs
-    GroupTile<T, S, TT, STATES> gt;
+    RowIn<T, VW, STATES> pu, pd, pz;
+    RowOut<T, VW> py;
+    pu.init(a.u, b, erow, a.T, c0 + ecol);
+    pd.init(a.delta, b, erow, a.T, c0 + ecol);
+    if (gated) pz.init(a.z, b, erow, a.T, c0 + ecol);
+    if (!STATES) py.init(a.y, b, erow, c0 + ecol);
+    GroupTile<T, S, TT, !STATES> gt;
+    gt.init(a, b, g, tid);
     auto load = [&](int t0) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int t = t0 + erow + v * PR;
             const int n = t < len && t < t_end ? en : 0;
-            raw_load(ru[v], a.u, b, t, a.T, c0 + ecol, n);
-            raw_load(rd[v], a.delta, b, t, a.T, c0 + ecol, n);
-            if (!STATES && a.z.p) raw_load(rz[v], a.z, b, t, a.T, c0 + ecol, n);
+            pu.load(ru[v], a.u, t0 + v * PR, c0 + ecol, n);
+            pd.load(rd[v], a.delta, t0 + v * PR, c0 + ecol, n);
+            if (gated) pz.load(rz[v], a.z, t0 + v * PR, c0 + ecol, n);
         }
-        gt.load(a, a.B, a.C, b, g, t0, min(len, t_end), tid);
+        gt.load(a, t0, min(len, t_end), tid);
     };
 
     load(t_begin);
@@ -120,18 +94,26 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
         for (int v = 0; v < NV; ++v) {
             const int r = erow + v * PR;
             const bool in = t0 + r < len && t0 + r < t_end;
-            float d[VW], z[VW];
+            float d[VW], pair[2 * VW];
             raw_get(ru[v], a.u, c0 + ecol, u[v]);
             raw_get(rd[v], a.delta, c0 + ecol, d);
-            if (!STATES && a.z.p) raw_get(rz[v], a.z, c0 + ecol, z);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) d[i] += bias[i];
+            if (a.softplus) {
+                float sig;
+#pragma unroll
+                for (int i = 0; i < VW; ++i) d[i] = softplus(d[i], sig);
+            }
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
-                float sig;
-                float x = d[i] + bias[i];
-                if (a.softplus) x = softplus(x, sig);
-                x = in && i < en ? x : 0.0f;
-                ds[r][ecol + i] = make_float2(x, x * u[v][i]);
-                gate[v][i] = !STATES && a.z.p ? z[i] * sigmoid(z[i]) : 1.0f;
+                pair[2 * i] = in ? d[i] : 0.0f;
+                pair[2 * i + 1] = pair[2 * i] * u[v][i];
+            }
+            lds_put(&ds[r][ecol].x, pair);
+            if (gated) {
+                raw_get(rz[v], a.z, c0 + ecol, gate[v]);
+#pragma unroll
+                for (int i = 0; i < VW; ++i) gate[v][i] *= sigmoid(gate[v][i]);
             }
         }
         gt.store(bc, tid);
@@ -167,8 +149,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
                     y = lanes_sum<S>(y);
                     // the sum is in all of the channel's lanes: each keeps one of R steps, for one store
                     ykeep = j % R == 0 || q == j % R ? y : ykeep;
-                    // the channel's lanes, all of one wave, have read these steps' pairs
-                    if (j % R == R - 1 && (S <= R || q < R)) ds[r - (R - 1) + q][ch].x = ykeep;
+                    if (j % R == R - 1 && (S <= R || q < R)) yl[r - (R - 1) + q][ch] = ykeep;
                 }
             }
         }
@@ -177,14 +158,19 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int r = erow + v * PR;
-                if (t0 + r >= t_end) continue;
                 float o[VW];
+                lds_get(&yl[r][ecol], o);
 #pragma unroll
-                for (int i = 0; i < VW; ++i)
-                    o[i] = t0 + r < len ? fmaf(Dv[i], u[v][i], ds[r][ecol + i].x) * gate[v][i] : 0.0f;
-                store_vec<T, VW>(a.y, b, t0 + r, c0 + ecol, en, o);
+                for (int i = 0; i < VW; ++i) o[i] = fmaf(Dv[i], u[v][i], o[i]);
+                if (gated)
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) o[i] *= gate[v][i];
+                const bool in = t0 + r < len;
+#pragma unroll
+                for (int i = 0; i < VW; ++i) o[i] = in ? o[i] : 0.0f;
+                if (t0 + r < t_end) py.store(a.y, t0 + v * PR, en, o);
             }
-            __syncthreads();
+            // the next tile's ds and bc are read by nobody yet, its yl is written after a barrier
         }
     }
     if (!live) return;

@@ -11,19 +11,11 @@
 // elementwise work are those of the forward kernel.  The sums over channels
 // are taken in three steps of fixed order: within a wave by lane swaps, over
 // the workgroup's waves in LDS, over workgroups by scan_sums_kernel.
-#include "seq_device.h"
+#include "seq_scan.h"
 
 namespace {
 
 constexpr int kAhead = 4;
-
-template <int S>
-struct BwdShape {
-    static constexpr int NP = 4 * S;
-    static constexpr int CB = S <= 4 ? 64 : S == 8 ? 32 : 16;
-    static constexpr int NT = CB * S;
-    static constexpr int WAVES = NT / 64;
-};
 
 __device__ __forceinline__ void swap_add32(float& a, float b) {
     // lower lanes: a of both halves, upper lanes: b of both halves
@@ -52,21 +44,23 @@ __device__ __forceinline__ float row_sum(float x) {
 // the elementwise work needs before and after them waits in LDS, so that two
 // waves fit on a SIMD.
 template <class T, int S, bool STATES, bool PK>
-__global__ void __launch_bounds__(BwdShape<S>::NT) __attribute__((amdgpu_waves_per_eu(S == 1 ? 1 : 2, S == 1 ? 1 : 2)))
+__global__ void __launch_bounds__(ScanShape<S>::NT) __attribute__((amdgpu_waves_per_eu(S == 1 ? 1 : 2, S == 1 ? 1 : 2)))
 scan_backward_kernel(ScanArgs a) {
-    constexpr int NP = BwdShape<S>::NP, CB = BwdShape<S>::CB, NT = BwdShape<S>::NT, TT = kScanSeg;
-    constexpr int W = BwdShape<S>::WAVES;
+    constexpr int NP = ScanShape<S>::NP, CB = ScanShape<S>::CB, NT = ScanShape<S>::NT, TT = kScanSeg;
+    constexpr int W = NT / 64;
     constexpr int EP = TT * CB / NT;
     constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
-    constexpr int BW = 2 * NP, BE = (TT * BW + NT - 1) / NT;
+    constexpr int BW = 2 * NP, SV = TT * BW / NT;   // shares of dB, dC that a thread sums
     constexpr int TK = STATES ? 1 : TT;
-    __shared__ float2 ds[TT][CB];                  // (delta', delta' u), then (s1, s2 / ln 2)
-    __shared__ float dyl[TT][CB];                  // dy'
-    __shared__ float yl[TK][CB];                   // sum_n C h
+    // (delta', delta' u), then (s1, s2 / ln 2); its padding, and yl's and red's, puts the four steps
+    // that a store writes on different banks
+    __shared__ __align__(16) float2 ds[TT][CB + 8];
+    __shared__ __align__(16) float dyl[TT][CB];    // dy'
+    __shared__ __align__(16) float yl[TK][CB + 16];   // sum_n C h
     __shared__ __align__(16) float ul[TK][CB], dl[TK][CB], sl[TK][CB], wl[TK][CB];   // u, delta', its slope, dy silu'(z)
-    __shared__ float pl[2][CB];                    // delta_bias, D
+    __shared__ __align__(16) float pl[2][CB];                    // delta_bias, D
     __shared__ __align__(16) float bc[TT * BW];
-    __shared__ float red[TK][W][BW];               // the waves' shares of dB, dC
+    __shared__ __align__(16) float red[TK][W * BW + 16];   // the waves' shares of dB, dC
 
     const int tid = threadIdx.x;
     const int nblk = a.groups * a.gblocks;
@@ -77,6 +71,7 @@ scan_backward_kernel(ScanArgs a) {
     const int t_begin = part * a.chunk_len, t_end = min(a.T, t_begin + a.chunk_len);
 
     const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
+    const bool gated = a.z.p;
     float sumD[VW], sumB[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) sumD[i] = sumB[i] = 0.0f;
@@ -103,6 +98,8 @@ scan_backward_kernel(ScanArgs a) {
     }
 
     constexpr int R = S < 4 ? S : 4, M = 16 / S < 4 ? 16 / S : 4;
+    float* bcout = STATES ? nullptr
+                          : a.bcpart + (((long long)b * a.T + tid * SV / BW) * nblk + blk) * BW + tid * SV % BW;
     const int copy = lane % 16 / S;
     const int at = (lane >> 5) * NP + 4 * q + 2 * ((lane >> 4) & 1);
     float k0 = 0.0f, k1 = 0.0f, m0 = 0.0f, m1 = 0.0f;
@@ -110,7 +107,20 @@ scan_backward_kernel(ScanArgs a) {
     // a tile's inputs as they lie in memory, loaded while the one behind it is worked on
     Raw<T, VW, PK> ru[NV], rd[NV], rz[NV];
     Raw<T, VW, false> ry[NV];
-    T rb[BE];
+    RowIn<T, VW, PK> pu, pd, pz;
+    RowIn<T, VW, false> py;
+    RowOut<T, VW> qu, qd, qz;
+    pu.init(a.u, b, erow, a.T, c0 + ecol);
+    pd.init(a.delta, b, erow, a.T, c0 + ecol);
+    py.init(a.dy, b, erow, a.T, c0 + ecol);
+    if (gated) pz.init(a.z, b, erow, a.T, c0 + ecol);
+    if (!STATES) {
+        qu.init(a.du, b, erow, c0 + ecol);
+        qd.init(a.ddelta, b, erow, c0 + ecol);
+        if (gated) qz.init(a.dz, b, erow, c0 + ecol);
+    }
+    GroupTile<T, S, TT, true> gt;
+    gt.init(a, b, g, tid);
     float4 h4;
     auto load = [&](int t0) {
         h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -121,20 +131,12 @@ scan_backward_kernel(ScanArgs a) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int t = t0 + erow + v * PR, n = t < len && t < t_end ? en : 0;
-            raw_load(ru[v], a.u, b, t, a.T, c0 + ecol, n);
-            raw_load(rd[v], a.delta, b, t, a.T, c0 + ecol, n);
-            raw_load(ry[v], a.dy, b, t, a.T, c0 + ecol, n);
-            if (a.z.p) raw_load(rz[v], a.z, b, t, a.T, c0 + ecol, n);
+            pu.load(ru[v], a.u, t0 + v * PR, c0 + ecol, n);
+            pd.load(rd[v], a.delta, t0 + v * PR, c0 + ecol, n);
+            py.load(ry[v], a.dy, t0 + v * PR, c0 + ecol, n);
+            if (gated) pz.load(rz[v], a.z, t0 + v * PR, c0 + ecol, n);
         }
-#pragma unroll
-        for (int e = 0; e < BE; ++e) {
-            const int i = e * NT + tid, t = t0 + i / BW, k = i % BW, n = k % NP;
-            rb[e] = T(0.0f);
-            if (i < TT * BW && t < len && t < t_end && n < a.state) {
-                const SeqT& s = k < NP ? a.B : a.C;
-                rb[e] = reinterpret_cast<const T*>(s.p)[b * s.sample + t * s.row + (long long)g * a.state + n];
-            }
-        }
+        gt.load(a, t0, min(len, t_end), tid);
     };
 
     const int last = t_begin + (t_end - 1 - t_begin) / TT * TT;
@@ -147,11 +149,10 @@ scan_backward_kernel(ScanArgs a) {
                 const float zero[VW] = {};
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
-                    const int t = t0 + erow + v * PR;
-                    if (t >= t_end) continue;
-                    store_vec<T, VW>(a.du, b, t, c0 + ecol, en, zero);
-                    store_vec<T, VW>(a.ddelta, b, t, c0 + ecol, en, zero);
-                    if (a.dz.p) store_vec<T, VW>(a.dz, b, t, c0 + ecol, en, zero);
+                    if (t0 + erow + v * PR >= t_end) continue;
+                    qu.store(a.du, t0 + v * PR, en, zero);
+                    qd.store(a.ddelta, t0 + v * PR, en, zero);
+                    if (gated) qz.store(a.dz, t0 + v * PR, en, zero);
                 }
             }
             if (t0 > t_begin) load(t0 - TT);
@@ -161,34 +162,42 @@ scan_backward_kernel(ScanArgs a) {
         for (int v = 0; v < NV; ++v) {
             const int r = erow + v * PR;
             const bool in = t0 + r < len && t0 + r < t_end;
-            float u[VW], d[VW], dy[VW], z[VW];
+            float u[VW], d[VW], dy[VW], sig[VW], pair[2 * VW];
             raw_get(ru[v], a.u, c0 + ecol, u);
             raw_get(rd[v], a.delta, c0 + ecol, d);
             raw_get(ry[v], a.dy, c0 + ecol, dy);
-            if (a.z.p) raw_get(rz[v], a.z, c0 + ecol, z);
+            lds_get(&pl[0][ecol], sig);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) d[i] += sig[i], sig[i] = 1.0f;
+            if (a.softplus)
+#pragma unroll
+                for (int i = 0; i < VW; ++i) d[i] = softplus(d[i], sig[i]);
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
-                float x = d[i] + pl[0][ecol + i], sig = 1.0f;
-                if (a.softplus) x = softplus(x, sig);
-                x = in && i < en ? x : 0.0f;
-                ds[r][ecol + i] = make_float2(x, x * u[i]);
-                float gate = 1.0f;
-                if (a.z.p) {
-                    const float p = sigmoid(z[i]);
-                    gate = z[i] * p;
-                    if (!STATES) wl[r][ecol + i] = dy[i] * (p * fmaf(z[i], 1.0f - p, 1.0f));
-                }
-                dyl[r][ecol + i] = dy[i] * gate;
-                if constexpr (!STATES) {
-                    ul[r][ecol + i] = u[i];
-                    dl[r][ecol + i] = x;
-                    sl[r][ecol + i] = in ? sig : 0.0f;
-                }
+                d[i] = in ? d[i] : 0.0f;
+                pair[2 * i] = d[i];
+                pair[2 * i + 1] = d[i] * u[i];
             }
-        }
+            lds_put(&ds[r][ecol].x, pair);
+            if constexpr (!STATES) {
+                lds_put(&ul[r][ecol], u);
+                lds_put(&dl[r][ecol], d);
+                lds_put(&sl[r][ecol], sig);
+            }
+            if (gated) {
+                float z[VW], w[VW];
+                raw_get(rz[v], a.z, c0 + ecol, z);
 #pragma unroll
-        for (int e = 0; e < BE; ++e)
-            if (e * NT + tid < TT * BW) bc[e * NT + tid] = (float)rb[e];
+                for (int i = 0; i < VW; ++i) {
+                    const float p = sigmoid(z[i]);
+                    w[i] = dy[i] * (p * fmaf(z[i], 1.0f - p, 1.0f));
+                    dy[i] *= z[i] * p;
+                }
+                if constexpr (!STATES) lds_put(&wl[r][ecol], w);
+            }
+            lds_put(&dyl[r][ecol], dy);
+        }
+        gt.store(bc, tid);
         const float4 hs = h4;
         __syncthreads();
         if (t0 > t_begin) load(t0 - TT);
@@ -269,8 +278,13 @@ scan_backward_kernel(ScanArgs a) {
                 m0 = r % M == M - 1 || copy == r % M ? dB[0] : m0;
                 m1 = r % M == M - 1 || copy == r % M ? dB[1] : m1;
                 if (r % M == 0 && (16 / S <= M || copy < M))
-                    *reinterpret_cast<float2*>(&red[r + copy][wave][at]) = make_float2(m0, m1);
-                if (r % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
+                    *reinterpret_cast<float2*>(&red[r + copy][wave * BW + at]) = make_float2(m0, m1);
+                if (r % kAhead == 0) {
+                    // dA's sums stay here: put off, they would keep 64 products alive
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(dA[k]));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
         __syncthreads();
@@ -278,30 +292,49 @@ scan_backward_kernel(ScanArgs a) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int r = erow + v * PR, t = t0 + r;
+                const bool in = t < len;
+                float u[VW], dyp[VW], D[VW], d[VW], sl_[VW], s[2 * VW], o[VW];
+                lds_get(&ul[r][ecol], u);
+                lds_get(&dyl[r][ecol], dyp);
+                lds_get(&pl[1][ecol], D);
+                lds_get(&dl[r][ecol], d);
+                lds_get(&sl[r][ecol], sl_);
+                lds_get(&ds[r][ecol].x, s);
                 if (t >= t_end) continue;
-                float du[VW], dd[VW], dz[VW];
 #pragma unroll
                 for (int i = 0; i < VW; ++i) {
-                    const int c = ecol + i;
-                    const bool in = t < len && i < en;
-                    const float2 s = ds[r][c];
-                    const float u = ul[r][c], dyp = dyl[r][c], D = pl[1][c];
-                    dz[i] = in && a.z.p ? wl[r][c] * fmaf(D, u, yl[r][c]) : 0.0f;
-                    du[i] = in ? fmaf(D, dyp, dl[r][c] * s.x) : 0.0f;
-                    dd[i] = in ? fmaf(u, s.x, s.y * kLn2) * sl[r][c] : 0.0f;
-                    sumD[i] = in ? fmaf(dyp, u, sumD[i]) : sumD[i];
-                    sumB[i] += dd[i];
+                    sumD[i] = fmaf(dyp[i], u[i], sumD[i]);
+                    o[i] = in ? fmaf(D[i], dyp[i], d[i] * s[2 * i]) : 0.0f;
                 }
-                store_vec<T, VW>(a.du, b, t, c0 + ecol, en, du);
-                store_vec<T, VW>(a.ddelta, b, t, c0 + ecol, en, dd);
-                if (a.dz.p) store_vec<T, VW>(a.dz, b, t, c0 + ecol, en, dz);
-            }
-            for (int i = tid; i < TT * BW; i += NT) {
-                const int r = i / BW, k = i % BW;
-                float x = red[r][0][k];
+                qu.store(a.du, t0 + v * PR, en, o);
+                if (gated) {
+                    float w[VW], y[VW];
+                    lds_get(&wl[r][ecol], w);
+                    lds_get(&yl[r][ecol], y);
 #pragma unroll
-                for (int w = 1; w < W; ++w) x += red[r][w][k];
-                if (t0 + r < t_end) a.bcpart[(((long long)b * a.T + t0 + r) * nblk + blk) * BW + k] = x;
+                    for (int i = 0; i < VW; ++i) o[i] = in ? w[i] * fmaf(D[i], u[i], y[i]) : 0.0f;
+                    qz.store(a.dz, t0 + v * PR, en, o);
+                }
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    o[i] = in ? fmaf(u[i], s[2 * i], s[2 * i + 1] * kLn2) * sl_[i] : 0.0f;
+                    sumB[i] += o[i];
+                }
+                qd.store(a.ddelta, t0 + v * PR, en, o);
+            }
+            const int r = tid * SV / BW, k = tid * SV % BW;
+            float x[SV], y[SV];
+            lds_get(&red[r][k], x);
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                lds_get(&red[r][w * BW + k], y);
+#pragma unroll
+                for (int i = 0; i < SV; ++i) x[i] += y[i];
+            }
+            if (t0 + r < t_end) {
+                float* to = bcout + (long long)t0 * nblk * BW;
+#pragma unroll
+                for (int i = 0; i < SV; i += 2) *reinterpret_cast<float2*>(to + i) = make_float2(x[i], x[i + 1]);
             }
         }
         __syncthreads();
@@ -406,8 +439,8 @@ __global__ void __launch_bounds__(256) scan_sums_kernel(ScanArgs a, int NP, int 
 
 template <class T, int S, bool PK>
 hipError_t passes(const ScanArgs& a, hipStream_t s) {
-    constexpr int NP = BwdShape<S>::NP;
-    const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(BwdShape<S>::NT);
+    constexpr int NP = ScanShape<S>::NP;
+    const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
     if (a.chunks > 1) {
         // the first part's start is nobody's end
         scan_backward_kernel<T, S, true, PK><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
