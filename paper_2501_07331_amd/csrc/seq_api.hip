@@ -27,15 +27,19 @@ struct OnDevice {
     }
 };
 
-// Parts of the time axis: a single one where there are workgroups for the
-// chip's 256 CUs without a division, since the parts' starts cost a second
-// pass over the inputs; otherwise as many as fill it twice, of at least 64
-// steps.  len: steps a part, whole tiles.
-void time_parts(int T, long long workgroups, int* parts, int* len) {
-    const long long want = workgroups >= 256 ? 1 : (512 + workgroups - 1) / workgroups;
+// Parts of the time axis.  The parts' starts cost a second pass over the
+// inputs, so the axis is divided only where its waves leave too many of the
+// chip's 1024 SIMDs empty, and then into as many parts as give each SIMD
+// `fill` waves.  Measured at 16 states, bf16: forward, 1200 waves (20 x 800 x
+// 900) 156 us whole and 138 divided, 1680 waves (28 x 500 x 900) 104 whole and
+// 128 divided; forward and backward, 1680 waves, 382 with a whole backward
+// and 451 with a divided one.  len: steps a part, whole tiles.
+constexpr int kFwdWaves = 1408, kBwdWaves = 1024, kFwdFill = 4, kBwdFill = 2;
+void time_parts(int T, long long waves, int enough, int fill, int* parts, int* len) {
+    const long long want = waves >= enough ? 1 : (1024 * fill + waves - 1) / waves;
     const int tiles = (T + kScanTile - 1) / kScanTile;
-    const int per = std::max(2, (int)((tiles + want - 1) / want));
-    *len = std::min(per, tiles) * kScanTile;
+    const int per = std::max(1, (int)((tiles + want - 1) / want));
+    *len = per * kScanTile;
     *parts = (T + *len - 1) / *len;
 }
 
@@ -45,7 +49,8 @@ struct snn_seq {
     snn_seq_opts o;
     hipStream_t stream;
     int device;
-    int np, gblocks, segs, parts, part_len;
+    int np, gblocks, segs;
+    int parts, part_len, bparts, bpart_len;   // forward and backward
     char* mem;                         // one allocation
     float *carry, *dsum;               // states between the parts of the time axis
     float *bcpart, *apart, *dpart;     // shares of the scan's gradients
@@ -137,7 +142,7 @@ int f32_arg(snn_seq* s, const void* p, const char* name, bool need) {
         if (rc_) return rc_;     \
     } while (0)
 
-void scan_sizes(const snn_seq* s, ScanArgs* k) {
+void scan_sizes(const snn_seq* s, bool back, ScanArgs* k) {
     k->batch = s->o.batch;
     k->T = s->o.T;
     k->channels = s->o.channels;
@@ -145,8 +150,8 @@ void scan_sizes(const snn_seq* s, ScanArgs* k) {
     k->groups = s->o.groups;
     k->per = s->o.channels / s->o.groups;
     k->gblocks = s->gblocks;
-    k->chunks = s->parts;
-    k->chunk_len = s->part_len;
+    k->chunks = back ? s->bparts : s->parts;
+    k->chunk_len = back ? s->bpart_len : s->part_len;
     k->segs = s->segs;
     k->carry = s->carry;
     k->dsum = s->dsum;
@@ -191,12 +196,14 @@ extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
     s->np = np;
     s->gblocks = gblocks;
     s->segs = (o->T + kScanSeg - 1) / kScanSeg;
-    time_parts(o->T, wgs, &s->parts, &s->part_len);
+    const long long waves = wgs * cb * np / 256;
+    time_parts(o->T, waves, kFwdWaves, kFwdFill, &s->parts, &s->part_len);
+    time_parts(o->T, waves, kBwdWaves, kBwdFill, &s->bparts, &s->bpart_len);
     // floats: the parts' carries; for training the shares of the gradients
     const bool train = o->flags & SNN_SEQ_TRAIN;
-    const size_t bp = (size_t)o->batch * s->parts, C = o->channels;
-    const size_t n_carry = s->parts > 1 ? bp * C * np : 0, n_dsum = s->parts > 1 ? bp * C : 0;
-    const size_t n_a = train ? bp * C * np : 0, n_d = train ? bp * 2 * C : 0;
+    const size_t C = o->channels, most = std::max(s->parts, train ? s->bparts : 1);
+    const size_t n_dsum = most > 1 ? o->batch * most * C : 0, n_carry = n_dsum * np;
+    const size_t n_a = train ? (size_t)o->batch * s->bparts * C * np : 0, n_d = train ? (size_t)o->batch * s->bparts * 2 * C : 0;
     const size_t n_bc = train ? (size_t)o->batch * o->T * o->groups * gblocks * 2 * np : 0;
     const size_t n_conv = train ? (size_t)o->batch * conv_tiles(o->T) * (o->taps + 1) * C : 0;
     auto round4 = [](size_t x) { return (x + 3) & ~(size_t)3; };
@@ -417,7 +424,7 @@ static int scan_args(snn_seq* s, const snn_seq_scan* c, int T, ScanArgs* a) {
     a->saved = c->saved;
     a->lengths = c->lengths;
     a->softplus = c->softplus != 0;
-    scan_sizes(s, a);
+    scan_sizes(s, false, a);
     return SNN_OK;
 }
 
@@ -494,8 +501,11 @@ extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
     a.dh0 = c->dh0;
     a.lengths = c->lengths;
     a.softplus = c->softplus != 0;
-    scan_sizes(s, &a);
-    if (!c->saved) SEQ_TRY(s, launch_scan_states(a, type, s->stream));
+    if (!c->saved) {
+        scan_sizes(s, false, &a);
+        SEQ_TRY(s, launch_scan_states(a, type, s->stream));
+    }
+    scan_sizes(s, true, &a);
     SEQ_TRY(s, launch_scan_backward(a, type, s->stream));
     return SNN_OK;
 }

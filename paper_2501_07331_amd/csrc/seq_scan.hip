@@ -196,11 +196,24 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, int NP) {
     const bool in = n < a.state;
     const float A2 = in ? a.A[(long long)c * a.state + n] * kLog2e : 0.0f;
     float h = in && a.h0 ? a.h0[(b * a.channels + c) * a.state + n] : 0.0f;
-    for (int k = 0; k < a.chunks; ++k) {
-        const long long at = (b * a.chunks + k) * a.channels + c;
-        const float end = k + 1 < a.chunks ? a.carry[at * NP + n] : 0.0f;
-        a.carry[at * NP + n] = h;
-        if (k + 1 < a.chunks) h = fmaf(exp2_fast(a.dsum[at] * A2), h, end);
+    const long long step = a.channels;
+    long long at = b * a.chunks * step + c;
+    // eight parts' values are loaded before the first is used: they do not wait for one another
+    for (int k = 0; k < a.chunks; k += 8) {
+        float end[8], sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool some = k + j + 1 < a.chunks;
+            end[j] = some ? a.carry[(at + j * step) * NP + n] : 0.0f;
+            sum[j] = some ? a.dsum[at + j * step] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (k + j >= a.chunks) break;
+            a.carry[(at + j * step) * NP + n] = h;
+            h = fmaf(exp2_fast(sum[j] * A2), h, end[j]);
+        }
+        at += 8 * step;
     }
 }
 

@@ -383,11 +383,22 @@ __global__ void __launch_bounds__(256) scan_join_back_kernel(ScanArgs a, int NP)
     const bool in = n < a.state;
     const float A2 = in ? a.A[(long long)c * a.state + n] * kLog2e : 0.0f;
     float g = in && a.dhT ? a.dhT[(b * a.channels + c) * a.state + n] : 0.0f;
-    for (int k = a.chunks - 1; k >= 0; --k) {
-        const long long at = (b * a.chunks + k) * a.channels + c;
-        const float start = k > 0 ? a.carry[at * NP + n] : 0.0f;
-        a.carry[at * NP + n] = g;
-        if (k > 0) g = fmaf(exp2_fast(a.dsum[at] * A2), g, start);
+    const long long step = a.channels;
+    for (int k = a.chunks - 1; k >= 0; k -= 8) {
+        const long long at = (b * a.chunks + k) * step + c;
+        float start[8], sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool some = k - j > 0;
+            start[j] = some ? a.carry[(at - j * step) * NP + n] : 0.0f;
+            sum[j] = some ? a.dsum[at - j * step] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (k - j < 0) break;
+            a.carry[(at - j * step) * NP + n] = g;
+            g = fmaf(exp2_fast(sum[j] * A2), g, start[j]);
+        }
     }
 }
 

@@ -88,18 +88,15 @@ def _bind(lib):
     return lib
 
 
-_TYPES = None
+_TYPES = {}
 
 
-def _dtype(t) -> int:
-    global _TYPES
-    if _TYPES is None:
+def _types():
+    """Element types by torch's, filled once torch is there."""
+    if not _TYPES:
         import torch
-        _TYPES = {torch.float32: SNN_F32, torch.bfloat16: SNN_BF16, torch.float16: SNN_F16}
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise ValueError(f"a sequence must be float32, bfloat16 or float16, got {t.dtype}") from None
+        _TYPES.update({torch.float32: SNN_F32, torch.bfloat16: SNN_BF16, torch.float16: SNN_F16})
+    return _TYPES
 
 
 class Packed:
@@ -147,40 +144,51 @@ class _Handle:
             stream = torch.cuda.current_stream()
         self.stream = stream
         self.device = stream.device
+        # a call costs a few microseconds on the host, so what it needs of torch is looked up here
+        self._index, self._raw = stream.device.index, stream.cuda_stream
+        self._current = torch._C._cuda_getCurrentRawStream
+        self._types = _types()
+        self._float, self._int = torch.float32, torch.int32
 
     def _f32(self, t, numel, name, need=False):
-        import torch
-        return self._vec(t, torch.float32, numel, name, need)
+        return self._vec(t, self._float, numel, name, need)
 
     def _vec(self, t, dtype, numel, name, need=False):
+        """The address of a contiguous tensor of numel elements."""
         if t is None:
             if need:
                 raise ValueError(f"{name} is needed")
             return None
-        self._on_device(t, name)
-        if t.dtype != dtype:
+        if t.get_device() != self._index:
+            raise self._elsewhere(t, name)
+        if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.numel() != numel:
             raise ValueError(f"{name} must hold {numel} elements, got {t.numel()}")
-        return C.c_void_p(t.data_ptr()) if numel else None
+        return t.data_ptr() or None
 
-    def _on_device(self, t, name):
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
+    def _elsewhere(self, t, name):
+        return ValueError(f"{name} is on {t.device}, the handle on {self.device}")
+
+    def _dtype(self, t, name):
+        d = self._types.get(t.dtype)
+        if d is None:
+            raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        return d
 
     def _call(self, f, *args):
-        import torch
-        cur = torch.cuda.current_stream(self.device)
-        other = cur.cuda_stream != self.stream.cuda_stream
-        if other:
-            if self.stream.cuda_stream == 0 and torch.cuda.is_current_stream_capturing():
+        if self._current(self._index) == self._raw:
+            rc = f(self._h, *args)
+        else:
+            import torch
+            cur = torch.cuda.current_stream(self.device)
+            if self._raw == 0 and torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("the handle is bound to the default stream, which cannot be captured: "
                                    "make it under the stream of the capture")
             self.stream.wait_stream(cur)
-        rc = f(self._h, *args)
-        if other:
+            rc = f(self._h, *args)
             cur.wait_stream(self.stream)
         if rc != SNN_OK:
             raise SNNError(rc, self._error(self._h).decode())
@@ -195,6 +203,9 @@ class _Handle:
             self.close()
         except Exception:
             pass
+
+
+_NONE = (None, None, 0, 0, 0)      # no sequence
 
 
 class SequenceLayer(_Handle):
@@ -234,71 +245,71 @@ class SequenceLayer(_Handle):
     # ---------------------------------------------------------------- arguments
 
     def _seq(self, t, name, n, rows=None, packed=False, need=True):
-        """A sequence argument; rows None: T, 0: a step's [batch][n]."""
+        """A sequence argument, as an snn_tensor's fields; rows None: T, 0: a
+        step's [batch][n]."""
         if t is None:
             if need:
                 raise ValueError(f"{name} is needed")
-            return snn_tensor()
-        rows = self.T if rows is None else rows
-        if isinstance(t, Packed):
+            return _NONE
+        if rows is None:
+            rows = self.T
+        want = (self.batch, rows, n) if rows else (self.batch, n)
+        if t.shape != want:
+            raise ValueError(f"{name} must be {list(want)}, got {list(t.shape)}")
+        if t.__class__ is Packed:
             if not packed:
                 raise ValueError(f"{name} must not be packed here")
-            if tuple(t.shape) != (self.batch, rows, n):
-                raise ValueError(f"{name} must be {[self.batch, rows, n]}, got {list(t.shape)}")
-            self._on_device(t, name)
-            return snn_tensor(t.data.data_ptr(), t.scale.data_ptr(), n, n * rows, SNN_E4M3)
-        self._on_device(t, name)
-        want = (self.batch, rows, n) if rows else (self.batch, n)
-        if tuple(t.shape) != want:
-            raise ValueError(f"{name} must be {list(want)}, got {list(t.shape)}")
-        if t.stride(-1) != 1 and n > 1:
+            if t.data.get_device() != self._index:
+                raise self._elsewhere(t, name)
+            return t.data.data_ptr(), t.scale.data_ptr(), n, n * rows, SNN_E4M3
+        if t.get_device() != self._index:
+            raise self._elsewhere(t, name)
+        stride = t.stride()
+        if stride[-1] != 1 and n > 1:
             raise ValueError(f"{name}: the last dimension must be contiguous")
-        return snn_tensor(t.data_ptr(), None, t.stride(1) if rows else n, t.stride(0), _dtype(t))
+        return t.data_ptr(), None, stride[1] if rows else n, stride[0], self._dtype(t, name)
 
     def _lengths(self, lengths):
-        import torch
-        return self._vec(lengths, torch.int32, self.batch, "lengths")
+        return self._vec(lengths, self._int, self.batch, "lengths")
 
     # ---------------------------------------------------------------- counts
 
     def bin_spikes(self, offsets, step, neuron, dst, factor: int = 1):
         """Counts of an input spike list (Network.forward's offsets, step,
         neuron) in bins of `factor` steps: dst [batch][ceil(T / factor)][n]."""
-        import torch
-        inp = snn_spikes_in(self._vec(offsets, torch.int32, self.batch + 1, "offsets", True),
-                            self._vec(step, torch.int32, neuron.numel(), "step", True),
-                            self._vec(neuron, torch.int32, neuron.numel(), "neuron", True), neuron.numel())
+        inp = snn_spikes_in(self._vec(offsets, self._int, self.batch + 1, "offsets", True),
+                            self._vec(step, self._int, neuron.numel(), "step", True),
+                            self._vec(neuron, self._int, neuron.numel(), "neuron", True), neuron.numel())
         d = self._binned(dst, factor)
         self._call(self._lib.snn_seq_bin_spikes, C.byref(inp), dst.shape[-1], int(factor), C.byref(d))
 
     def bin_records(self, count, step, neuron, dst, factor: int = 1):
         """The same of one layer's spike records (count [batch], step and
         neuron [batch][capacity])."""
-        import torch
         if step.dim() != 2 or step.shape[0] != self.batch:
             raise ValueError("step must be [batch][capacity]")
-        rec = snn_spikes_out(self._vec(count, torch.int32, self.batch, "count", True),
-                             self._vec(step, torch.int32, step.numel(), "step", True),
-                             self._vec(neuron, torch.int32, step.numel(), "neuron", True))
+        rec = snn_spikes_out(self._vec(count, self._int, self.batch, "count", True),
+                             self._vec(step, self._int, step.numel(), "step", True),
+                             self._vec(neuron, self._int, step.numel(), "neuron", True))
         d = self._binned(dst, factor)
         self._call(self._lib.snn_seq_bin_records, C.byref(rec), step.shape[1], dst.shape[-1], int(factor), C.byref(d))
 
     def _binned(self, dst, factor):
         if factor < 1 or factor > self.T:
             raise ValueError(f"factor must be 1 .. {self.T}")
-        return self._seq(dst, "dst", dst.shape[-1], rows=-(-self.T // int(factor)))
+        return snn_tensor(*self._seq(dst, "dst", dst.shape[-1], rows=-(-self.T // int(factor))))
 
     # ---------------------------------------------------------------- packed form
 
     def pack(self, x, q: Packed):
         """q: the 8-bit form of x [batch][T][n] (any n)."""
         n = x.shape[-1]
-        a, b = self._seq(x, "x", n), self._seq(q, "q", n, packed=True)
+        a, b = snn_tensor(*self._seq(x, "x", n)), snn_tensor(*self._seq(q, "q", n, packed=True))
         self._call(self._lib.snn_seq_pack, n, C.byref(a), C.byref(b))
 
     def unpack(self, q: Packed, x):
         n = x.shape[-1]
-        a, b = self._seq(x, "x", n), self._seq(q, "q", n, packed=True)
+        a, b = snn_tensor(*self._seq(x, "x", n)), snn_tensor(*self._seq(q, "q", n, packed=True))
         self._call(self._lib.snn_seq_unpack, n, C.byref(b), C.byref(a))
 
     # ---------------------------------------------------------------- convolution
@@ -420,13 +431,13 @@ class Sampler(_Handle):
         (fp32), top_k (int32) hold a value for each row, or None: 1, all, 0,
         all.  logprob [rows]: the drawn classes' log-probabilities among
         those that the filters keep."""
-        import torch
         if scores.dim() != 2 or (scores.stride(1) != 1 and scores.shape[1] > 1):
             raise ValueError("scores must be [rows][n] with a contiguous last dimension")
-        self._on_device(scores, "scores")
+        if scores.get_device() != self._index:
+            raise self._elsewhere(scores, "scores")
         R, n = scores.shape
-        a = snn_sample_args(scores.data_ptr(), scores.stride(0), _dtype(scores), R, n, self._f32(u, R, "u", True),
-                            self._f32(temperature, R, "temperature"), self._vec(top_k, torch.int32, R, "top_k"),
+        a = snn_sample_args(scores.data_ptr(), scores.stride(0), self._dtype(scores, "scores"), R, n, self._f32(u, R, "u", True),
+                            self._f32(temperature, R, "temperature"), self._vec(top_k, self._int, R, "top_k"),
                             self._f32(top_p, R, "top_p"), self._f32(min_p, R, "min_p"),
-                            self._vec(token, torch.int32, R, "token", True), self._f32(logprob, R, "logprob"))
+                            self._vec(token, self._int, R, "token", True), self._f32(logprob, R, "logprob"))
         self._call(self._lib.snn_sampler_sample, C.byref(a))
