@@ -515,6 +515,7 @@ extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
 struct snn_sampler {
     int rows, n, device;
     hipStream_t stream;
+    char* scratch;
     char err[512];
 };
 
@@ -540,6 +541,15 @@ extern "C" int snn_sampler_create(int32_t rows, int32_t n, void* hip_stream, snn
     s->n = n;
     s->device = dev;
     s->stream = static_cast<hipStream_t>(hip_stream);
+    const size_t bytes = sample_scratch(rows, n);
+    if (bytes) {
+        const hipError_t m = hipMalloc(reinterpret_cast<void**>(&s->scratch), bytes);
+        if (m != hipSuccess) {
+            (void)hipGetLastError();
+            free(s);
+            return create_fail(m == hipErrorOutOfMemory ? SNN_ENOMEM : SNN_EDEVICE, "hipMalloc", hipGetErrorString(m));
+        }
+    }
     *out = s;
     return SNN_OK;
 }
@@ -551,6 +561,7 @@ extern "C" void snn_sampler_destroy(snn_sampler* s) {
     {
         OnDevice on(s->device);
         (void)hipStreamSynchronize(s->stream);
+        if (s->scratch) (void)hipFree(s->scratch);
     }
     free(s);
 }
@@ -579,6 +590,9 @@ extern "C" int snn_sampler_sample(snn_sampler* s, const snn_sample_args* c) {
     a.n = c->n;
     a.shift = 62;
     while ((1ll << (62 - a.shift)) < c->n) --a.shift;
+    a.parts = sample_parts(c->rows, c->n);
+    a.part_len = ((c->n + a.parts - 1) / a.parts + 7) & ~7;
+    a.scratch = s->scratch;
     a.u = c->u;
     a.temperature = c->temperature;
     a.top_k = c->top_k;

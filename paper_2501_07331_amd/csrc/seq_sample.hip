@@ -14,6 +14,13 @@
 // limits is passed, and again inside that interval over equal parts of its
 // keys, until a part is a single key.  The draw then goes over the row once
 // in index order.
+//
+// Three ways by size.  Rows of up to kWaveRow scores: a wave a row, an element
+// ranked by comparing it with every other.  Long rows that are too few to
+// fill the chip: a row is divided among workgroups for everything that reads
+// all of it, in five launches.  Otherwise a workgroup a row.
+#include <algorithm>
+
 #include "seq_device.h"
 #include "seq_sample.h"
 
@@ -21,6 +28,7 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr int kBins = 2048;
+constexpr int kList = 1024;                        // most elements of an interval that are ranked one by one
 
 // NaN orders below everything, as -inf.
 __device__ __forceinline__ unsigned key_of(float z) {
@@ -56,47 +64,104 @@ __device__ u64 share(u64 a, float f, bool up) {
 }
 
 // A row's parameters, with their defaults and limits.
-struct RowArgs {
-    float temperature, min_p, u;
-    float top_p;
+struct Row {
+    float m, temperature, min_p, top_p, u;
     int top_k;
-};
-__device__ __forceinline__ RowArgs row_args(const SampleArgs& a, int row) {
-    RowArgs r;
-    const float t = a.temperature ? a.temperature[row] : 1.0f;
-    r.temperature = t == t ? t : 1.0f;
-    const float q = a.min_p ? a.min_p[row] : 0.0f;
-    r.min_p = q > 0.0f ? fminf(q, 1.0f) : 0.0f;
-    const float p = a.top_p ? a.top_p[row] : 1.0f;
-    r.top_p = p == p ? p : 1.0f;
-    const int k = a.top_k ? a.top_k[row] : 0;
-    r.top_k = k > 0 ? k : 0x7fffffff;
-    const float u = a.u[row];
-    r.u = u >= 0.0f ? fminf(u, 1.0f - 0x1p-24f) : 0.0f;
-    return r;
-}
+    double inverse;                                // of the temperature
+    float bins;                                    // intervals of depth per unit of score
+    int shift;
 
-// (m - z) / temperature: 0 for the largest scores, infinite ones among them.
-__device__ __forceinline__ double depth64(float m, float z, float temperature) {
-    if (z == m) return 0.0;
-    return m == INFINITY ? (double)INFINITY : ((double)m - (double)z) / (double)temperature;
-}
-// its interval: a function that never falls as z falls
-__device__ __forceinline__ int bin_of(float m, float z, float temperature) {
-    const float x = z == m ? 0.0f : (m - z) / temperature * 64.0f;
-    return (int)fminf(x, (float)(kBins - 1));
-}
+    __device__ __forceinline__ Row(const SampleArgs& a, int row) {
+        const float t = a.temperature ? a.temperature[row] : 1.0f;
+        temperature = t == t ? t : 1.0f;
+        const float q = a.min_p ? a.min_p[row] : 0.0f;
+        min_p = q > 0.0f ? fminf(q, 1.0f) : 0.0f;
+        const float p = a.top_p ? a.top_p[row] : 1.0f;
+        top_p = p == p ? p : 1.0f;
+        const int k = a.top_k ? a.top_k[row] : 0;
+        top_k = k > 0 ? k : 0x7fffffff;
+        const float v = a.u[row];
+        u = v >= 0.0f ? fminf(v, 1.0f - 0x1p-24f) : 0.0f;
+        inverse = 1.0 / (double)temperature;
+        bins = 64.0f / temperature;
+        shift = a.shift;
+        m = 0.0f;
+    }
+    // (m - z) / temperature: 0 for the largest scores, infinite ones among them
+    __device__ __forceinline__ double depth(float z) const {
+        if (z == m) return 0.0;
+        return m == INFINITY ? (double)INFINITY : ((double)m - (double)z) * inverse;
+    }
+    // its interval: a function that never falls as z falls
+    __device__ __forceinline__ int bin(float z) const {
+        const float x = z == m ? 0.0f : (m - z) * bins;
+        return (int)fminf(x, (float)(kBins - 1));
+    }
+    // The weight 2^shift exp(-depth), rounded to a whole number; kept: whether
+    // min-p keeps it.  exp by reduction to |y| <= ln 2 / 2 with ln 2 in two
+    // parts and the series to y^12, whose remainder is below 2e-16.
+    __device__ __forceinline__ u64 weight(float z, bool& kept) const {
+        const double x = depth(z), n = rint(x * 1.4426950408889634);
+        double y = fma(n, 0x1.62e42fee00000p-1, -x);
+        y = fma(n, 0x1.a39ef35793c76p-33, y);
+        double p = 1.0 / 479001600.0;
+        p = fma(p, y, 1.0 / 39916800.0);
+        p = fma(p, y, 1.0 / 3628800.0);
+        p = fma(p, y, 1.0 / 362880.0);
+        p = fma(p, y, 1.0 / 40320.0);
+        p = fma(p, y, 1.0 / 5040.0);
+        p = fma(p, y, 1.0 / 720.0);
+        p = fma(p, y, 1.0 / 120.0);
+        p = fma(p, y, 1.0 / 24.0);
+        p = fma(p, y, 1.0 / 6.0);
+        p = fma(p, y, 0.5);
+        p = fma(p, y, 1.0);
+        p = fma(p, y, 1.0);
+        const bool tiny = !(x < 700.0);            // exp(-700) is 0 in every unit; NaN cannot be
+        const double w = tiny ? 0.0 : ldexp(p, -(int)n);
+        kept = w >= (double)min_p;
+        return (u64)rint(ldexp(w, shift));
+    }
+    __device__ __forceinline__ u64 mass_limit(u64 all) const {
+        return top_p >= 1.0f ? ~0ull : top_p > 0.0f ? max((u64)1, share(all, top_p, true)) : 1;
+    }
+    __device__ __forceinline__ float logprob(float z, u64 total) const {
+        return (float)(-depth(z) - log(ldexp((double)total, -shift)));
+    }
+};
 
 template <class T, int VW>
-__device__ __forceinline__ void load_scores(const SampleArgs& a, int row, int i, float (&z)[VW]) {
+__device__ __forceinline__ void load_scores(const SampleArgs& a, int row, int i, int end, float (&z)[VW]) {
     const T* p = reinterpret_cast<const T*>(a.scores) + (long long)row * a.row + i;
-    if (i + VW <= a.n) {
+    if (i + VW <= end) {
         const typename Vec<T, VW>::type v = *reinterpret_cast<const typename Vec<T, VW>::type*>(p);
 #pragma unroll
         for (int j = 0; j < VW; ++j) z[j] = (float)v[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < VW; ++j) z[j] = i + j < a.n ? (float)p[j] : -INFINITY;
+        for (int j = 0; j < VW; ++j) z[j] = i + j < end ? (float)p[j] : -INFINITY;
+    }
+}
+template <class T>
+constexpr int scores_vw() { return sizeof(T) == 4 ? 4 : 8; }
+
+// f(index, score) for the elements of [begin, end) of a row, kBatch vectors of
+// a thread loaded before the first is looked at.
+template <class T, int NT, int kBatch, class F>
+__device__ __forceinline__ void each_score(const SampleArgs& a, int row, int begin, int end, F f) {
+    constexpr int VW = scores_vw<T>();
+    for (int base = begin + threadIdx.x * VW; base < end; base += NT * VW * kBatch) {
+        float z[kBatch][VW];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (base + k * NT * VW < end) load_scores<T, VW>(a, row, base + k * NT * VW, end, z[k]);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+            for (int j = 0; j < VW; ++j) {
+                const int i = base + k * NT * VW + j;
+                if (i < end) f(i, z[k][j]);
+            }
     }
 }
 
@@ -116,246 +181,611 @@ __device__ __forceinline__ V wave_sum(V x) {
     for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
     return x;
 }
+__device__ __forceinline__ unsigned wave_max(unsigned x) {
+#pragma unroll
+    for (int d = 32; d; d /= 2) x = max(x, (unsigned)__shfl_xor((int)x, d));
+    return x;
+}
+
+// What a workgroup of NT threads works on a row with.
+template <int NT>
+struct Work {
+    u64 mass[kBins];
+    unsigned count[kBins];
+    unsigned list[kList];
+    u64 wmass[NT / 64];
+    unsigned wcount[NT / 64];
+    u64 above, inside_mass;        // weight above the cut interval, and of it
+    unsigned n_above, inside;      // elements above it, and in it
+    unsigned lo, hi, ends[3];      // its keys
+    int bin, listed, token;
+    static_assert(kList <= kBins, "the list's weights take the histogram's place");
+};
+
+// Largest key of [begin, end) of a row, in every thread.
+template <class T, int NT>
+__device__ unsigned top_key(const SampleArgs& a, int row, int begin, int end, Work<NT>& w) {
+    const int tid = threadIdx.x;
+    unsigned top = 0;
+    each_score<T, NT, 4>(a, row, begin, end, [&](int, float z) { top = max(top, key_of(z)); });
+    top = wave_max(top);
+    if (tid % 64 == 0) w.wcount[tid / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) top = max(top, w.wcount[k]);
+    __syncthreads();
+    return top;
+}
+
+// First index of [begin, end) with key `top`, or end; in every thread.
+template <class T, int NT>
+__device__ int first_index(const SampleArgs& a, int row, int begin, int end, unsigned top, Work<NT>& w) {
+    if (threadIdx.x == 0) w.token = end;
+    __syncthreads();
+    int first = end;
+    each_score<T, NT, 4>(a, row, begin, end, [&](int i, float z) { first = key_of(z) == top ? min(first, i) : first; });
+    if (first < end) atomicMin(&w.token, first);
+    __syncthreads();
+    return w.token;
+}
+
+// The histogram of [begin, end) over the intervals of depth, and the weight of
+// all of it (returned in every thread).
+template <class T, int NT>
+__device__ u64 depth_histogram(const SampleArgs& a, int row, int begin, int end, const Row& r, Work<NT>& w) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < kBins; i += NT) w.mass[i] = 0, w.count[i] = 0;
+    __syncthreads();
+    u64 sum = 0;
+    each_score<T, NT, NT == 1024 ? 1 : 2>(a, row, begin, end, [&](int, float z) {
+        if (!(z > -INFINITY)) return;              // NaN too
+        bool kept;
+        const u64 v = r.weight(z, kept);
+        sum += v;
+        if (!kept) return;
+        const int b = r.bin(z);
+        if (v) atomicAdd(&w.mass[b], v);
+        atomicAdd(&w.count[b], 1u);
+    });
+    sum = wave_sum(sum);
+    if (tid % 64 == 0) w.wmass[tid / 64] = sum;
+    __syncthreads();
+    u64 all = 0;
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) all += w.wmass[k];
+    return all;
+}
+
+// The first interval of the histogram at whose end a limit is reached or
+// passed; kBins if none.  w.above ... w.inside follow it.
+template <int NT>
+__device__ int find_cut(Work<NT>& w, u64 above, unsigned n_above, u64 limit, unsigned top_k) {
+    constexpr int PB = kBins / NT;
+    const int tid = threadIdx.x, wave = tid / 64;
+    if (tid == 0) w.bin = kBins;
+    u64 tm = 0;
+    unsigned tc = 0;
+#pragma unroll
+    for (int j = 0; j < PB; ++j) tm += w.mass[tid * PB + j], tc += w.count[tid * PB + j];
+    const u64 sm = wave_scan(tm);
+    const unsigned sc = wave_scan(tc);
+    __syncthreads();
+    if (tid % 64 == 63) w.wmass[wave] = sm, w.wcount[wave] = sc;
+    __syncthreads();
+    u64 bm = above + sm - tm;
+    unsigned bc = n_above + sc - tc;
+    for (int k = 0; k < wave; ++k) bm += w.wmass[k], bc += w.wcount[k];
+    const u64 bm0 = bm;
+    const unsigned bc0 = bc;
+#pragma unroll
+    for (int j = 0; j < PB; ++j) {
+        const int b = tid * PB + j;
+        // one interval passes them: at its start they are not, at its end they are
+        const bool before = bc <= top_k && bm < limit;
+        bm += w.mass[b], bc += w.count[b];
+        if (before && w.count[b] && (bc > top_k || bm >= limit)) w.bin = b;
+    }
+    __syncthreads();
+    const int cb = w.bin;
+    if (cb == kBins) {
+        if (tid == NT - 1) w.above = bm, w.n_above = bc;
+    } else if (cb / PB == tid) {
+        bm = bm0, bc = bc0;
+        for (int b = tid * PB; b < cb; ++b) bm += w.mass[b], bc += w.count[b];
+        w.above = bm, w.n_above = bc;
+        w.inside_mass = w.mass[cb], w.inside = w.count[cb];
+    }
+    __syncthreads();
+    return cb;
+}
+
+// Where a row's kept elements end: those with a key above `key`, and the
+// first `count` of those that have it; `mass`: their weight.
+struct End {
+    unsigned key, count;
+    u64 mass;
+};
+
+// The end in `inside` elements of one key: as many as the limits leave.
+__device__ __forceinline__ End end_in_key(const Row& r, unsigned key, unsigned inside, u64 inside_mass, u64 above,
+                                          unsigned n_above, u64 limit) {
+    unsigned count = min(inside, (unsigned)r.top_k - n_above);
+    const u64 one = inside_mass / inside;
+    if (above >= limit) count = 0;
+    else if (one) count = (unsigned)min((u64)count, (limit - above - 1) / one + 1);
+    return End{key, count, above + one * count};
+}
+
+// From the histogram over the intervals of depth, for [0, n) of the row.
+template <class T, int NT>
+__device__ End find_end(const SampleArgs& a, int row, const Row& r, unsigned top, u64 limit, Work<NT>& w) {
+    const int tid = threadIdx.x;
+    u64 above = 0;
+    unsigned n_above = 0, lo = kNegInf + 1, hi = top;
+    int sh = 0;
+    for (int level = 0;; ++level) {
+        const int cb = find_cut(w, above, n_above, limit, (unsigned)r.top_k);
+        above = w.above, n_above = w.n_above;
+        if (cb == kBins) return End{0, 0, above};  // nothing is cut off
+        const unsigned inside = w.inside;
+        const u64 inside_mass = w.inside_mass;
+        if (tid == 0) w.listed = 0;
+        if (level) {
+            if (tid == 0) {
+                w.hi = hi - ((unsigned)cb << sh);
+                w.lo = max(lo, w.hi - ((1u << sh) - 1));
+            }
+        } else if (tid < 192) {
+            // The keys of an interval of depth, which falls as keys rise: the
+            // least with bin <= cb (first wave) and the least with bin < cb,
+            // whose predecessor is the largest (second wave), and the least that
+            // min-p keeps (third), 64 candidates a round; x is the answer's
+            // lower bound, y an upper one.
+            const int lane = tid % 64, most = tid < 64 ? cb : cb - 1;
+            auto holds = [&](unsigned k) {
+                bool kept;
+                if (tid < 128) return r.bin(score_of(k)) <= most;
+                r.weight(score_of(k), kept);
+                return kept;
+            };
+            unsigned x = lo, y = hi + 1;           // hi itself has bin 0; hi + 1 stands for none
+            while (x < y) {
+                const unsigned step = (y - x) / 64 + 1, k = x + lane * step;
+                const u64 in = __ballot(k < y), yes = __ballot(k < y && holds(k));
+                // the answer lies after the last candidate that says no, up to the first that says yes
+                const int first = yes ? __ffsll(yes) - 1 : __popcll(in);
+                if (yes) y = x + first * step;
+                if (first) x += (first - 1) * step + 1;
+            }
+            if (lane == 0) w.ends[tid / 64] = tid / 64 == 1 ? x - 1 : x;
+        }
+        __syncthreads();
+        // kept elements only, as in the histogram
+        lo = level ? w.lo : max(w.ends[0], w.ends[2]), hi = level ? w.hi : w.ends[1];
+        if (lo == hi) return end_in_key(r, lo, inside, inside_mass, above, n_above, limit);
+        const float zlo = score_of(lo), zhi = score_of(hi);
+        if (inside <= kList) {
+            // few elements: each is placed by comparison with all of them
+            each_score<T, NT, 4>(a, row, 0, a.n, [&](int, float z) {
+                if (!(z >= zlo && z <= zhi)) return;
+                const int at = atomicAdd(&w.listed, 1);
+                if (at < kList) w.list[at] = key_of(z);     // always: they are the interval's `inside`
+            });
+            __syncthreads();
+            for (unsigned e = tid; e < inside; e += NT) {
+                bool kept;
+                w.mass[e] = r.weight(score_of(w.list[e]), kept);
+            }
+            __syncthreads();
+            // G neighbouring lanes an element, each over its share of the list
+            const unsigned G = inside <= NT / 16 ? 16 : inside <= NT / 4 ? 4 : 1;
+            for (unsigned e = tid / G; e < inside; e += NT / G) {
+                const unsigned key = w.list[e];
+                u64 bm = 0, em = 0;
+                unsigned bc = 0, ec = 0;
+#pragma unroll 4
+                for (unsigned i = tid % G; i < inside; i += G) {
+                    const unsigned other = w.list[i];
+                    const u64 v = w.mass[i];
+                    bm += other > key ? v : 0, bc += other > key;
+                    em += other == key ? v : 0, ec += other == key;
+                }
+                for (unsigned d = 1; d < G; d *= 2) {
+                    bm += __shfl_xor(bm, d), em += __shfl_xor(em, d);
+                    bc += __shfl_xor(bc, d), ec += __shfl_xor(ec, d);
+                }
+                bm += above, bc += n_above;
+                const unsigned k = (unsigned)r.top_k;
+                // the limits are passed among this key's elements; they all find the same
+                if (bc <= k && bm < limit && (bc + ec > k || bm + em >= limit)) {
+                    w.lo = key, w.above = bm, w.n_above = bc;
+                    w.inside = ec, w.inside_mass = em;
+                }
+            }
+            __syncthreads();
+            return end_in_key(r, w.lo, w.inside, w.inside_mass, w.above, w.n_above, limit);
+        }
+        sh = 0;
+        while ((hi - lo) >> sh >= (unsigned)kBins) ++sh;
+        for (int i = tid; i < kBins; i += NT) w.mass[i] = 0, w.count[i] = 0;
+        __syncthreads();
+        each_score<T, NT, NT == 1024 ? 2 : 4>(a, row, 0, a.n, [&](int, float z) {
+            if (!(z >= zlo && z <= zhi)) return;
+            bool kept;
+            const u64 v = r.weight(z, kept);
+            const int b = (int)((hi - key_of(z)) >> sh);
+            if (v) atomicAdd(&w.mass[b], v);
+            atomicAdd(&w.count[b], 1u);
+        });
+        __syncthreads();
+    }
+}
+
+// Weight of the kept elements of a thread's VW of the row from i on, those
+// with the last key counted in `ties` instead.
+template <class T, int VW>
+__device__ __forceinline__ void kept_weights(const float (&z)[VW], int i, int end, const Row& r, unsigned last, u64 (&v)[VW],
+                                             u64& mass, unsigned& ties) {
+#pragma unroll
+    for (int j = 0; j < VW; ++j) {
+        v[j] = 0;
+        const unsigned key = i + j < end ? key_of(z[j]) : 0;
+        if (key <= kNegInf || key < last) continue;
+        bool kept;
+        const u64 x = r.weight(z[j], kept);
+        if (!kept) continue;
+        v[j] = x;
+        if (key == last) ties += 1; else mass += x;
+    }
+}
+
+// The first index of [begin, end) whose running sum is above `goal`, from a
+// running sum `run` and `ties` elements with the last key before begin.
+template <class T, int NT>
+__device__ void draw(const SampleArgs& a, int row, int begin, int end, const Row& r, const End& e, u64 goal, u64 run,
+                     unsigned ties, Work<NT>& w) {
+    constexpr int VW = scores_vw<T>(), W = NT / 64;
+    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+    for (int base = begin; base < end && run <= goal; base += NT * VW) {
+        const int i = base + tid * VW;
+        float z[VW];
+        u64 v[VW], tm = 0;
+        unsigned tc = 0;
+        if (i < end) load_scores<T, VW>(a, row, i, end, z);
+        kept_weights<T, VW>(z, i, end, r, e.key, v, tm, tc);
+        const unsigned sc = wave_scan(tc);
+        __syncthreads();
+        if (lane == 63) w.wcount[wave] = sc;
+        __syncthreads();
+        unsigned before = ties + sc - tc;
+        for (int k = 0; k < wave; ++k) before += w.wcount[k];
+        for (int k = 0; k < W; ++k) ties += w.wcount[k];
+        // of the elements with the last key the first e.count by index
+#pragma unroll
+        for (int j = 0; j < VW; ++j) {
+            const unsigned key = i + j < end ? key_of(z[j]) : 0;
+            if (e.key && key == e.key && v[j]) {
+                if (before >= e.count) v[j] = 0;
+                ++before;
+                tm += v[j];
+            }
+        }
+        const u64 sm = wave_scan(tm);
+        if (lane == 63) w.wmass[wave] = sm;
+        __syncthreads();
+        u64 at = run + sm - tm;
+        for (int k = 0; k < wave; ++k) at += w.wmass[k];
+        for (int k = 0; k < W; ++k) run += w.wmass[k];
+        if (at <= goal && at + tm > goal) {        // one thread of the row
+            int token = 0;
+            float zt = 0.0f;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) {
+                if (at <= goal && at + v[j] > goal) token = j, zt = z[j];
+                at += v[j];
+            }
+            a.token[row] = i + token;
+            if (a.logprob) a.logprob[row] = r.logprob(zt, e.mass);
+        }
+    }
+}
+
+__device__ __forceinline__ void answer(const SampleArgs& a, int row, int token, float logprob) {
+    a.token[row] = token;
+    if (a.logprob) a.logprob[row] = logprob;
+}
 
 template <class T, int NT>
 __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a) {
-    constexpr int VW = sizeof(T) == 4 ? 4 : 8, W = NT / 64, PB = kBins / NT;
-    __shared__ u64 mass[kBins];
-    __shared__ unsigned count[kBins];
-    __shared__ u64 wmass[W];
-    __shared__ unsigned wcount[W];
-    __shared__ struct {
-        u64 mass, below;           // weight above the cut; that of the cut interval
-        unsigned count, inside;    // elements above the cut; in the cut interval
-        unsigned lo, hi;           // keys of the cut interval
-        int bin, token;
-    } cut;
-    const int row = blockIdx.x, tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-    const RowArgs r = row_args(a, row);
-
-    // the largest score, as its key
-    unsigned top = 0;
-    for (int i = tid * VW; i < a.n; i += NT * VW) {
-        float z[VW];
-        load_scores<T, VW>(a, row, i, z);
-#pragma unroll
-        for (int j = 0; j < VW; ++j) top = max(top, i + j < a.n ? key_of(z[j]) : 0u);
-    }
-#pragma unroll
-    for (int d = 32; d; d /= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
-    if (lane == 0) wcount[wave] = top;
-    if (tid == 0) cut.token = a.n;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) top = max(top, wcount[w]);
-    const float m = score_of(top);
+    __shared__ Work<NT> w;
+    const int row = blockIdx.x;
+    Row r(a, row);
+    const unsigned top = top_key<T, NT>(a, row, 0, a.n, w);
     if (top <= kNegInf) {
-        if (tid == 0) {
-            a.token[row] = -1;
-            if (a.logprob) a.logprob[row] = -INFINITY;
-        }
+        if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
         return;
     }
+    r.m = score_of(top);
     if (!(r.temperature > 0.0f)) {
-        int first = a.n;
-        for (int i = tid * VW; i < a.n && first == a.n; i += NT * VW) {
-            float z[VW];
-            load_scores<T, VW>(a, row, i, z);
-#pragma unroll
-            for (int j = VW - 1; j >= 0; --j)
-                if (i + j < a.n && key_of(z[j]) == top) first = i + j;
-        }
-        atomicMin(&cut.token, first);
-        __syncthreads();
-        if (tid == 0) {
-            a.token[row] = cut.token;
-            if (a.logprob) a.logprob[row] = 0.0f;
-        }
+        const int first = first_index<T, NT>(a, row, 0, a.n, top, w);
+        if (threadIdx.x == 0) answer(a, row, first, 0.0f);
         return;
     }
+    const u64 all = depth_histogram<T, NT>(a, row, 0, a.n, r, w);
+    const End e = find_end<T, NT>(a, row, r, top, r.mass_limit(all), w);
+    draw<T, NT>(a, row, 0, a.n, r, e, share(e.mass, r.u, false), 0, 0, w);
+}
 
-    const double unit = ldexp(1.0, a.shift);
-    // the weight of a score that is kept by min-p; total gets every weight
-    auto weigh = [&](float z, u64* total) {
-        const double w = exp(-depth64(m, z, r.temperature));
-        const u64 v = (u64)rint(w * unit);
-        if (total) *total += v;
-        return w >= (double)r.min_p ? v : ~0ull;
-    };
-
-    u64 all = 0, limit = 0;
-    u64 above = 0;                 // weight and number of the elements above the interval
-    unsigned n_above = 0;
-    unsigned lo = kNegInf + 1, hi = top;   // the interval's keys
-    unsigned end_key = 0, end_count = 0;   // where the kept ones end
-    u64 kept = 0;                  // their weight
-    for (int level = 0;; ++level) {
-        int sh = 0;
-        while ((hi - lo) >> sh >= (unsigned)kBins) ++sh;
-        for (int i = tid; i < kBins; i += NT) mass[i] = 0, count[i] = 0;
-        __syncthreads();
-        u64 sum = 0;
-        for (int i = tid * VW; i < a.n; i += NT * VW) {
-            float z[VW];
-            load_scores<T, VW>(a, row, i, z);
+// A wave a row of at most 64 * E scores: an element's place in falling order
+// and the weight before it by comparison with all of them.
+template <class T, int E>
+__global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
+    const int row = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+    if (row >= a.rows) return;
+    Row r(a, row);
+    float z[E];
+    unsigned key[E], top = 0;
+    const T* p = reinterpret_cast<const T*>(a.scores) + (long long)row * a.row;
 #pragma unroll
-            for (int j = 0; j < VW; ++j) {
-                const unsigned key = key_of(z[j]);
-                if (key < lo || key > hi) continue;
-                const u64 w = weigh(z[j], &sum);
-                if (w == ~0ull) continue;
-                const int b = level ? (int)((hi - key) >> sh) : bin_of(m, z[j], r.temperature);
-                atomicAdd(&mass[b], w);
-                atomicAdd(&count[b], 1u);
-            }
-        }
-        if (level == 0) {
-            sum = wave_sum(sum);
-            if (lane == 0) wmass[wave] = sum;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < W; ++w) all += wmass[w];
-            limit = r.top_p >= 1.0f ? ~0ull : r.top_p > 0.0f ? max((u64)1, share(all, r.top_p, true)) : 1;
-        }
-        if (tid == 0) cut.bin = kBins;
-        __syncthreads();
-        // running sums over the intervals, PB a thread
-        u64 tm = 0;
-        unsigned tc = 0;
-#pragma unroll
-        for (int j = 0; j < PB; ++j) tm += mass[tid * PB + j], tc += count[tid * PB + j];
-        const u64 sm = wave_scan(tm);
-        const unsigned sc = wave_scan(tc);
-        if (lane == 63) wmass[wave] = sm, wcount[wave] = sc;
-        __syncthreads();
-        u64 bm = above + sm - tm;
-        unsigned bc = n_above + sc - tc;
-        for (int w = 0; w < wave; ++w) bm += wmass[w], bc += wcount[w];
-#pragma unroll
-        for (int j = 0; j < PB; ++j) {
-            const int b = tid * PB + j;
-            const u64 em = bm + mass[b];
-            const unsigned ec = bc + count[b];
-            // the first interval at whose end a limit is reached or passed
-            if (count[b] && (ec > (unsigned)r.top_k || em >= limit)) atomicMin(&cut.bin, b);
-            bm = em, bc = ec;
-        }
-        __syncthreads();
-        const int cb = cut.bin;
-        if (cb / PB == tid || (cb == kBins && tid == NT - 1)) {
-            // bm, bc are the sums at the end of this thread's intervals: back to the cut's start
-            u64 x = bm;
-            unsigned y = bc;
-            if (cb < kBins)
-                for (int b = (tid + 1) * PB - 1; b >= cb; --b) x -= mass[b], y -= count[b];
-            cut.mass = x, cut.count = y;
-            cut.below = cb < kBins ? mass[cb] : 0;
-            cut.inside = cb < kBins ? count[cb] : 0;
-        }
-        if (tid == 0 && cb < kBins) {
-            if (level) {
-                cut.hi = hi - ((unsigned)cb << sh);
-                cut.lo = max(lo, cut.hi - ((1u << sh) - 1));
-            } else {
-                // the keys of an interval of depth: its ends by bisection
-                unsigned x = lo, y = hi;           // the least key with bin <= cb
-                while (x < y) {
-                    const unsigned k = x + (y - x) / 2;
-                    if (bin_of(m, score_of(k), r.temperature) <= cb) y = k; else x = k + 1;
-                }
-                cut.lo = x;
-                y = hi;                            // the largest with bin >= cb
-                while (x < y) {
-                    const unsigned k = y - (y - x) / 2;
-                    if (bin_of(m, score_of(k), r.temperature) >= cb) x = k; else y = k - 1;
-                }
-                cut.hi = x;
-            }
-        }
-        __syncthreads();
-        above = cut.mass, n_above = cut.count;
-        if (cb == kBins) {                         // nothing is cut off
-            end_key = 0;
-            kept = above;
-            break;
-        }
-        lo = cut.lo, hi = cut.hi;
-        if (lo == hi) {
-            // a single key: as many as the limits leave
-            end_key = lo;
-            end_count = min(cut.inside, (unsigned)r.top_k - n_above);
-            const u64 w = cut.below / cut.inside;
-            if (above >= limit) end_count = 0;
-            else if (w) end_count = (unsigned)min((u64)end_count, (limit - above - 1) / w + 1);
-            kept = above + w * end_count;
-            break;
-        }
-        __syncthreads();                           // cut is written again
+    for (int j = 0; j < E; ++j) {
+        const int i = j * 64 + lane;
+        z[j] = i < a.n ? (float)p[i] : -INFINITY;
+        key[j] = i < a.n ? key_of(z[j]) : 0u;
+        top = max(top, key[j]);
     }
-
-    // the draw: the first index whose running sum is above u times the total
-    const u64 goal = share(kept, r.u, false);
+    top = wave_max(top);
+    if (top <= kNegInf) {
+        if (lane == 0) answer(a, row, -1, -INFINITY);
+        return;
+    }
+    r.m = score_of(top);
+    if (!(r.temperature > 0.0f)) {
+        int first = -1;
+#pragma unroll
+        for (int j = E - 1; j >= 0; --j) {
+            const u64 has = __ballot(key[j] == top);
+            if (has) first = j * 64 + __ffsll((unsigned long long)has) - 1;
+        }
+        if (lane == 0) answer(a, row, first, 0.0f);
+        return;
+    }
+    u64 v[E], all = 0;
+    bool kept[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        v[j] = 0, kept[j] = false;
+        if (key[j] > kNegInf) v[j] = r.weight(z[j], kept[j]);
+        all += v[j];
+    }
+    all = wave_sum(all);
+    const u64 limit = r.mass_limit(all);
+    if (r.top_k < a.n || limit != ~0ull) {
+        u64 before[E] = {};
+        unsigned rank[E] = {};
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int n = min(64, a.n - 64 * k);
+            for (int l = 0; l < n; ++l) {
+                const unsigned other = (unsigned)__builtin_amdgcn_readlane((int)key[k], l);
+                const u64 weight = (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)v[k], l) |
+                                   (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v[k] >> 32), l) << 32;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const bool is_before = other > key[j] || (other == key[j] && (k < j || (k == j && l < lane)));
+                    before[j] += is_before ? weight : 0;
+                    rank[j] += is_before;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) kept[j] = kept[j] && rank[j] < (unsigned)r.top_k && before[j] < limit;
+    }
+    u64 total = 0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        v[j] = kept[j] ? v[j] : 0;
+        total += v[j];
+    }
+    total = wave_sum(total);
+    const u64 goal = share(total, r.u, false);
     u64 run = 0;
-    unsigned ties = 0;
-    for (int base = 0; base < a.n; base += NT * VW) {
-        const int i = base + tid * VW;
-        float z[VW];
-        u64 w[VW], tm = 0;
-        unsigned tc = 0;
-        if (i < a.n) load_scores<T, VW>(a, row, i, z);
 #pragma unroll
-        for (int j = 0; j < VW; ++j) {
-            w[j] = 0;
-            const unsigned key = i + j < a.n ? key_of(z[j]) : 0;
-            if (key <= kNegInf || key < end_key) continue;
-            const u64 v = weigh(z[j], nullptr);
-            if (v == ~0ull) continue;
-            w[j] = v;
-            if (key == end_key) tc += 1; else tm += v;
-        }
-        const unsigned sc = wave_scan(tc);
-        __syncthreads();
-        if (lane == 63) wcount[wave] = sc;
-        __syncthreads();
-        unsigned before = ties + sc - tc;
-        for (int k = 0; k < wave; ++k) before += wcount[k];
-        for (int k = 0; k < W; ++k) ties += wcount[k];
-        // of the elements with the last key the first end_count by index
-#pragma unroll
-        for (int j = 0; j < VW; ++j) {
-            const unsigned key = i + j < a.n ? key_of(z[j]) : 0;
-            if (end_key && key == end_key && w[j]) {
-                if (before >= end_count) w[j] = 0;
-                ++before;
-                tm += w[j];
-            }
-        }
-        const u64 sm = wave_scan(tm);
-        if (lane == 63) wmass[wave] = sm;
-        __syncthreads();
-        u64 at = run + sm - tm;
-        for (int k = 0; k < wave; ++k) at += wmass[k];
-        for (int k = 0; k < W; ++k) run += wmass[k];
-        if (at <= goal && at + tm > goal) {        // one thread of the row
-            int token = 0;
-#pragma unroll
-            for (int j = 0; j < VW; ++j) {
-                if (at <= goal && at + w[j] > goal) token = j;
-                at += w[j];
-            }
-            a.token[row] = i + token;
-            float zt = z[0];
-#pragma unroll
-            for (int j = 1; j < VW; ++j) zt = token == j ? z[j] : zt;
-            if (a.logprob) a.logprob[row] = (float)(-depth64(m, zt, r.temperature) - log((double)kept / unit));
-        }
-        if (run > goal) break;
+    for (int j = 0; j < E; ++j) {
+        const u64 s = run + wave_scan(v[j]);
+        if (s - v[j] <= goal && s > goal) answer(a, row, j * 64 + lane, r.logprob(z[j], total));
+        run = __shfl(s, 63);
     }
+}
+
+// ------------------------------------------------------------------ rows divided among workgroups
+
+constexpr int kPartNT = 256;
+
+// What the launches of a divided row hand on: [rows] of
+struct RowState {
+    u64 all, goal, end_mass;
+    unsigned top, end_key, end_count;
+    int done;                      // answered already
+};
+struct PartState {                 // [rows][parts]
+    u64 all, mass;                 // weight, and that of the kept elements above the last key
+    unsigned top, ties;
+};
+
+__device__ __forceinline__ RowState* row_state(const SampleArgs& a) { return reinterpret_cast<RowState*>(a.scratch); }
+__device__ __forceinline__ PartState* part_state(const SampleArgs& a) {
+    return reinterpret_cast<PartState*>(row_state(a) + a.rows);
+}
+__device__ __forceinline__ u64* hist_mass(const SampleArgs& a) {
+    return reinterpret_cast<u64*>(part_state(a) + (long long)a.rows * a.parts);
+}
+__device__ __forceinline__ unsigned* hist_count(const SampleArgs& a) {
+    return reinterpret_cast<unsigned*>(hist_mass(a) + (long long)a.rows * kBins);
+}
+
+// Largest keys; the row's histogram is cleared.
+template <class T>
+__global__ void __launch_bounds__(kPartNT) sample_top_kernel(SampleArgs a) {
+    __shared__ Work<kPartNT> w;
+    const int part = blockIdx.x, row = blockIdx.y;
+    const int begin = part * a.part_len, end = min(a.n, begin + a.part_len);
+    const unsigned top = top_key<T, kPartNT>(a, row, begin, end, w);
+    if (threadIdx.x == 0) part_state(a)[row * a.parts + part].top = top;
+    for (int i = part * kPartNT + threadIdx.x; i < kBins; i += a.parts * kPartNT) {
+        hist_mass(a)[(long long)row * kBins + i] = 0;
+        hist_count(a)[(long long)row * kBins + i] = 0;
+    }
+}
+
+__device__ __forceinline__ unsigned row_top(const SampleArgs& a, int row) {
+    unsigned top = 0;
+    for (int k = threadIdx.x % 64; k < a.parts; k += 64) top = max(top, part_state(a)[row * a.parts + k].top);
+    return wave_max(top);
+}
+
+// Histograms of the parts, added to the row's.
+template <class T>
+__global__ void __launch_bounds__(kPartNT) sample_hist_kernel(SampleArgs a) {
+    __shared__ Work<kPartNT> w;
+    const int part = blockIdx.x, row = blockIdx.y;
+    const int begin = part * a.part_len, end = min(a.n, begin + a.part_len);
+    Row r(a, row);
+    const unsigned top = row_top(a, row);
+    if (top <= kNegInf || !(r.temperature > 0.0f)) return;
+    r.m = score_of(top);
+    const u64 all = depth_histogram<T, kPartNT>(a, row, begin, end, r, w);
+    if (threadIdx.x == 0) part_state(a)[row * a.parts + part].all = all;
+    for (int i = threadIdx.x; i < kBins; i += kPartNT) {
+        if (!w.count[i]) continue;
+        if (w.mass[i]) atomicAdd(&hist_mass(a)[(long long)row * kBins + i], w.mass[i]);
+        atomicAdd(&hist_count(a)[(long long)row * kBins + i], w.count[i]);
+    }
+}
+
+// Where the kept elements end.
+template <class T>
+__global__ void __launch_bounds__(1024) sample_end_kernel(SampleArgs a) {
+    __shared__ Work<1024> w;
+    const int row = blockIdx.x, tid = threadIdx.x;
+    Row r(a, row);
+    RowState& s = row_state(a)[row];
+    const unsigned top = row_top(a, row);
+    if (tid == 0) s.top = top, s.done = top <= kNegInf || !(r.temperature > 0.0f);
+    if (top <= kNegInf) {
+        if (tid == 0) answer(a, row, -1, -INFINITY);
+        return;
+    }
+    r.m = score_of(top);
+    if (!(r.temperature > 0.0f)) {
+        const int first = first_index<T, 1024>(a, row, 0, a.n, top, w);
+        if (tid == 0) answer(a, row, first, 0.0f);
+        return;
+    }
+    u64 all = 0;
+    for (int k = tid % 64; k < a.parts; k += 64) all += part_state(a)[row * a.parts + k].all;
+    all = wave_sum(all);
+    for (int i = tid; i < kBins; i += 1024) {
+        w.mass[i] = hist_mass(a)[(long long)row * kBins + i];
+        w.count[i] = hist_count(a)[(long long)row * kBins + i];
+    }
+    __syncthreads();
+    const End e = find_end<T, 1024>(a, row, r, top, r.mass_limit(all), w);
+    if (tid == 0) {
+        s.end_key = e.key, s.end_count = e.count, s.end_mass = e.mass;
+        s.goal = share(e.mass, r.u, false);
+    }
+}
+
+// The parts' kept weight.
+template <class T>
+__global__ void __launch_bounds__(kPartNT) sample_parts_kernel(SampleArgs a) {
+    __shared__ u64 mass[kPartNT / 64];
+    __shared__ unsigned ties[kPartNT / 64];
+    const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    const int begin = part * a.part_len, end = min(a.n, begin + a.part_len);
+    const RowState s = row_state(a)[row];
+    if (s.done) return;
+    Row r(a, row);
+    r.m = score_of(s.top);
+    u64 m = 0;
+    unsigned t = 0;
+    const float last = s.end_key ? score_of(s.end_key) : -INFINITY;
+    each_score<T, kPartNT, 2>(a, row, begin, end, [&](int, float z) {
+        if (!(z >= last && z > -INFINITY)) return;
+        if (z == last) {
+            ++t;                                   // min-p keeps the last key: the end is among what it keeps
+            return;
+        }
+        bool kept;
+        const u64 v = r.weight(z, kept);
+        m += kept ? v : 0;
+    });
+    m = wave_sum(m), t = wave_sum(t);
+    if (tid % 64 == 0) mass[tid / 64] = m, ties[tid / 64] = t;
+    __syncthreads();
+    if (tid) return;
+    for (int k = 1; k < kPartNT / 64; ++k) m += mass[k], t += ties[k];
+    PartState& p = part_state(a)[row * a.parts + part];
+    p.mass = m, p.ties = t;
+}
+
+// The part in which the running sum passes the goal, and the index in it.
+template <class T>
+__global__ void __launch_bounds__(kPartNT) sample_draw_kernel(SampleArgs a) {
+    __shared__ Work<kPartNT> w;
+    const int row = blockIdx.x;
+    const RowState s = row_state(a)[row];
+    if (s.done) return;
+    Row r(a, row);
+    r.m = score_of(s.top);
+    const End e{s.end_key, s.end_count, s.end_mass};
+    u64 run = 0, one = 0;
+    unsigned ties = 0;
+    if (e.key) {
+        bool kept;
+        one = r.weight(score_of(e.key), kept);
+    }
+    // sums up to each part: the weight above the last key, and as many of that key's as are kept
+    int part = a.parts - 1;
+    u64 mass = 0;
+    for (int base = 0; base < a.parts; base += 64) {
+        const int k = base + threadIdx.x % 64;
+        const PartState p = k < a.parts ? part_state(a)[row * a.parts + k] : PartState{};
+        const u64 m1 = mass + wave_scan(p.mass);
+        const unsigned t1 = ties + wave_scan(p.ties);
+        const u64 to = __ballot(k < a.parts && m1 + one * min(t1, e.count) > s.goal);
+        const int f = to ? __ffsll(to) - 1 : 63;
+        const u64 m0 = __shfl(m1 - p.mass, f);
+        const unsigned t0 = __shfl(t1 - p.ties, f);
+        if (to) {
+            part = base + f;
+            mass = m0, ties = t0;
+            break;
+        }
+        mass = __shfl(m1, 63), ties = __shfl(t1, 63);
+    }
+    run = mass + one * min(ties, e.count);
+    const int begin = part * a.part_len;
+    draw<T, kPartNT>(a, row, begin, min(a.n, begin + a.part_len), r, e, s.goal, run, ties, w);
 }
 
 template <class T>
 hipError_t sample(const SampleArgs& a, hipStream_t s) {
-    if (a.n <= 4096)
+    const unsigned waves = (a.rows + 3) / 4;
+    if (a.n <= 64)
+        sample_wave_kernel<T, 1><<<waves, 256, 0, s>>>(a);
+    else if (a.n <= 128)
+        sample_wave_kernel<T, 2><<<waves, 256, 0, s>>>(a);
+    else if (a.n <= 256)
+        sample_wave_kernel<T, 4><<<waves, 256, 0, s>>>(a);
+    else if (a.parts > 1) {
+        const dim3 grid(a.parts, a.rows);
+        sample_top_kernel<T><<<grid, kPartNT, 0, s>>>(a);
+        sample_hist_kernel<T><<<grid, kPartNT, 0, s>>>(a);
+        sample_end_kernel<T><<<a.rows, 1024, 0, s>>>(a);
+        sample_parts_kernel<T><<<grid, kPartNT, 0, s>>>(a);
+        sample_draw_kernel<T><<<a.rows, kPartNT, 0, s>>>(a);
+    } else if (a.n <= 4096)
         sample_row_kernel<T, 256><<<a.rows, 256, 0, s>>>(a);
     else
         sample_row_kernel<T, 1024><<<a.rows, 1024, 0, s>>>(a);
@@ -363,6 +793,19 @@ hipError_t sample(const SampleArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Workgroups of 2048 scores and more, where the rows alone give fewer
+// workgroups than half the chip's CUs.
+constexpr int kPartRows = 128, kPartAll = 1024, kPartScores = 2048, kPartMin = 16384;
+int sample_parts(int rows, int n) {
+    if (n < kPartMin || rows > kPartRows) return 1;
+    return std::min(n / kPartScores, kPartAll / rows);
+}
+size_t sample_scratch(int rows, int n) {
+    if (n < kPartMin) return 0;
+    const size_t r = std::min(rows, kPartRows);    // and rows x parts is at most kPartAll
+    return r * (sizeof(RowState) + kBins * 12) + kPartAll * sizeof(PartState);
+}
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t s) {
     SEQ_BY_TYPE(dtype, T, return sample<T>(a, s));

@@ -34,7 +34,7 @@ def _run(z, u, dtype, strided=False, **kw):
         assert (lp[r] == wlp) or abs(lp[r] - wlp) <= 2.0 ** -24 * abs(wlp) + half + 1e-12, (r, lp[r], wlp)
 
 
-@pytest.mark.parametrize("V", [1, 2, 20, 63, 257, 1000, 4097, 9001])
+@pytest.mark.parametrize("V", [1, 2, 20, 63, 64, 65, 128, 200, 256, 257, 1000, 4097, 9001, 16384, 20011])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
 def test_every_filter(V, dtype):
     r = np.random.default_rng(V)
@@ -59,7 +59,7 @@ def test_one_filter_at_a_time(V):
     _run(z, u, "float32", temperature=[0.0, -1.0, 1e-30, 1e-3, 1e30, np.inf, 1.0, 0.5, 2.0])
 
 
-@pytest.mark.parametrize("V", [7, 256, 4500])
+@pytest.mark.parametrize("V", [7, 100, 256, 300, 4500, 17001])
 def test_ties_are_cut_by_index(V):
     """Rows of one value, and of three: the limits fall inside values that many classes share.  Weights of 1 have exact
     sums, so a border that top-p meets is met exactly."""
@@ -74,17 +74,18 @@ def test_ties_are_cut_by_index(V):
     _run(z, u, "bfloat16", top_k=np.full(R, max(1, V // 2)), top_p=r.uniform(0.2, 0.9, R))
 
 
-def test_values_that_are_no_scores():
+@pytest.mark.parametrize("V", [40, 150, 600, 5000, 16400])
+def test_values_that_are_no_scores(V):
     r = np.random.default_rng(3)
-    z = r.normal(size=(9, 40)).astype(np.float32)
+    z = r.normal(size=(9, V)).astype(np.float32)
     z[0] = -np.inf
     z[1] = np.nan
     z[2, ::3] = np.nan
     z[3, 5] = z[3, 9] = np.inf
-    z[4, :39] = -np.inf
+    z[4, :V - 1] = -np.inf
     z[5] = np.finfo(np.float32).min
     z[6, 0], z[6, 1] = np.finfo(np.float32).max, np.finfo(np.float32).min
-    z[7] = np.float32(1e-45) * np.arange(40)
+    z[7] = np.float32(1e-45) * np.arange(V)
     z[8, 3] = np.inf
     z[8, 4:] = np.nan
     u = r.random(9)
@@ -94,7 +95,7 @@ def test_values_that_are_no_scores():
     nan = np.full(9, np.nan)
     import torch
     import paper_2501_07331_amd as snn
-    s = snn.Sampler(9, 40)
+    s = snn.Sampler(9, V)
     f = lambda v: torch.tensor(v, dtype=torch.float32, device="cuda")   # noqa: E731
     a, b = torch.empty(9, dtype=torch.int32, device="cuda"), torch.empty(9, dtype=torch.int32, device="cuda")
     s.sample(f(z), f(np.zeros(9)), a)
@@ -113,6 +114,49 @@ def test_a_long_row_and_the_ends_of_u():
     u = [0.0, 1 - 2.0 ** -24, 0.5, 2.0 ** -30, 0.999, 0.25]
     _run(z, u, "float32")
     _run(z, u, "bfloat16", top_p=np.full(6, 0.95), top_k=[0, 0, 1000, 60000, 12345, 0])
+
+
+def test_a_handle_serves_smaller_calls():
+    """Rows and scores below the handle's: a row is divided otherwise for each call."""
+    import torch
+    import paper_2501_07331_amd as snn
+    r = np.random.default_rng(12)
+    s = snn.Sampler(200, 40000)
+    for R, V in ((200, 40000), (128, 16384), (7, 40000), (1, 33333), (3, 70), (90, 16383)):
+        z, u = r.normal(size=(R, V)).astype(np.float32) * 2, r.random(R).astype(np.float32)
+        p = r.uniform(0.5, 1, R).astype(np.float32)
+        t, token = torch.from_numpy(z).cuda(), torch.empty(R, dtype=torch.int32, device="cuda")
+        s.sample(t, torch.from_numpy(u).cuda(), token, top_p=torch.from_numpy(p).cuda())
+        got = token.cpu().numpy()
+        for i in range(0, R, max(1, R // 10)):
+            assert got[i] == seq.sample(z[i], float(u[i]), top_p=float(p[i]))[0], (R, V, i)
+
+
+def test_draws_in_a_graph():
+    """Replayed on new scores and numbers: every replay equals the eager call (the divided row's histograms are cleared by each)."""
+    import torch
+    import paper_2501_07331_amd as snn
+    r = np.random.default_rng(13)
+    R, V = 4, 20000
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        s, eager = snn.Sampler(R, V), snn.Sampler(R, V)
+        z, u = torch.zeros(R, V, device="cuda"), torch.zeros(R, device="cuda")
+        p = torch.full((R,), 0.9, device="cuda")
+        token = torch.empty(R, dtype=torch.int32, device="cuda")
+        want = torch.empty_like(token)
+        s.sample(z, u, token, top_p=p)
+        st.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            s.sample(z, u, token, top_p=p)
+        for _ in range(4):
+            z.copy_(torch.from_numpy(r.normal(size=(R, V)).astype(np.float32) * 3))
+            u.copy_(torch.from_numpy(r.random(R).astype(np.float32)))
+            g.replay()
+            eager.sample(z, u, want, top_p=p)
+            st.synchronize()
+            assert torch.equal(token, want)
 
 
 def test_the_network_answers():
