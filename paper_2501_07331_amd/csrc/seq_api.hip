@@ -205,7 +205,7 @@ extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
     const size_t n_dsum = most > 1 ? o->batch * most * C : 0, n_carry = n_dsum * np;
     const size_t n_a = train ? (size_t)o->batch * s->bparts * C * np : 0, n_d = train ? (size_t)o->batch * s->bparts * 2 * C : 0;
     const size_t n_bc = train ? (size_t)o->batch * o->T * o->groups * gblocks * 2 * np : 0;
-    const size_t n_conv = train ? (size_t)o->batch * conv_tiles(o->T) * (o->taps + 1) * C : 0;
+    const size_t n_conv = train ? (size_t)o->batch * conv_tiles(o->T, o->channels, o->taps) * (o->taps + 1) * C : 0;
     auto round4 = [](size_t x) { return (x + 3) & ~(size_t)3; };
     const size_t n_states = o->flags & SNN_SEQ_RECOMPUTE ? (size_t)o->batch * s->segs * C * np : 0;
     const size_t n_scan = round4(n_carry) + round4(n_dsum) + round4(n_a) + round4(n_d) + round4(n_bc) + n_states;
@@ -343,7 +343,6 @@ static int conv_args(snn_seq* s, const snn_seq_conv* c, int T, ConvArgs* a) {
     a->channels = C;
     a->taps = s->o.taps;
     a->silu = c->silu != 0;
-    a->tiles = conv_tiles(T);
     return SNN_OK;
 }
 
@@ -392,7 +391,7 @@ extern "C" int snn_seq_conv_backward(snn_seq* s, const snn_seq_conv_grad* c) {
     a.channels = C;
     a.taps = s->o.taps;
     a.silu = c->silu != 0;
-    a.tiles = conv_tiles(T);
+    a.tiles = conv_tiles(T, C, s->o.taps);
     a.part = s->cpart;
     SEQ_TRY(s, launch_conv_backward(a, type, s->stream));
     return SNN_OK;

@@ -1,22 +1,29 @@
 // Short causal convolution of each channel with its own taps, and SiLU.
 //
-// Bound by memory: a thread takes VW neighbouring channels (a 16-byte vector)
-// over kConvRun steps and keeps the window of inputs in registers, so that
-// every input is read once but for the window at a run's start.  The backward
-// pass goes over the same run in the same order: the pre-activation is made
-// again from x, and dx[t] leaves when the last output that read x[t] is done,
-// taps - 1 steps later.
+// Bound by memory: a thread takes four neighbouring channels over a run of
+// steps and keeps the window of inputs in registers, so that every input is
+// read once but for the window at a run's start.  The rows of a batch of
+// steps are loaded while the batch before it is worked on: what is in flight,
+// not the width of a load, carries the bandwidth.  The backward pass goes over
+// the same run in the same order: the pre-activation is made again from x, and
+// dx[t] leaves when the last output that read x[t] is done, taps - 1 steps
+// later.
 #include "seq_device.h"
 
 namespace {
 
-constexpr int kConvRun = 16;      // steps of a thread
-constexpr int kConvLanes = 16;    // threads side by side along the channels
-constexpr int kConvRows = 16;     // threads along the time axis
+constexpr int kConvVW = 4;        // channels of a thread
+constexpr int kConvThreads = 256; // of a workgroup: lanes x rows, lanes along the channels
+constexpr int kConvBatches = 4;   // of a run
 
-// channels of a thread: 8, or 4 where many taps' windows fill the registers
 template <int K>
-constexpr int conv_vw() { return K <= 4 ? 8 : 4; }
+constexpr int conv_batch() { return K <= 4 ? 8 : 4; }
+// steps of a run: the backward's goes taps - 1 steps further, to the end of a batch
+template <int K>
+constexpr int conv_run(bool back) { return kConvBatches * conv_batch<K>() - (back ? K - 1 : 0); }
+int conv_run(int taps, bool back) { return kConvBatches * (taps <= 4 ? 8 : 4) - (back ? taps - 1 : 0); }
+// 32 threads side by side along the channels, or 16 where that is all of them
+int conv_lanes(int channels) { return channels <= 16 * kConvVW ? 16 : 32; }
 
 __device__ __forceinline__ void dsilu(float x, float& y, float& dy) {
     const float p = sigmoid(x);
@@ -40,14 +47,24 @@ __device__ __forceinline__ void conv_in(const ConvArgs& a, int b, int t, int len
 }
 
 template <class T, int K>
-__global__ void __launch_bounds__(kConvLanes * kConvRows) conv_forward_kernel(ConvArgs a) {
-    constexpr int VW = conv_vw<K>();
-    const int c = (blockIdx.x * kConvLanes + threadIdx.x % kConvLanes) * VW, n = a.channels - c;
+__global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(ConvArgs a) {
+    constexpr int VW = kConvVW, NB = conv_batch<K>(), RUN = conv_run<K>(false);
+    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * VW, n = a.channels - c;
     const int b = blockIdx.z;
-    const int t0 = (blockIdx.y * kConvRows + threadIdx.x / kConvLanes) * kConvRun;
+    const int t0 = (blockIdx.y * blockDim.y + threadIdx.y) * RUN;
     if (n <= 0 || t0 >= a.T) return;
-    const int len = clamp_len(a.lengths, b, a.T);
-    float w[K][VW], bias[VW], x[K][VW];
+    const int len = clamp_len(a.lengths, b, a.T), t_end = min(a.T, t0 + RUN);
+    RowIn<T, VW, false> px;
+    RowOut<T, VW> py;
+    px.init(a.x, b, t0, a.T, c);
+    py.init(a.y, b, t0, c);
+    Raw<T, VW, false> raw[NB];
+    auto load = [&](int j0) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) px.load(raw[j], a.x, j0 + j, c, t0 + j0 + j < len ? n : 0);
+    };
+    load(0);
+    float w[K][VW], bias[VW], x[K - 1 + NB][VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
         bias[i] = a.bias && i < n ? a.bias[c + i] : 0.0f;
@@ -56,25 +73,32 @@ __global__ void __launch_bounds__(kConvLanes * kConvRows) conv_forward_kernel(Co
     }
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) conv_in<T, VW, false>(a, b, t0 - (K - 1) + k, len, c, n, x[k]);
+#pragma unroll 1
+    for (int j0 = 0; t0 + j0 < t_end; j0 += NB) {
 #pragma unroll
-    for (int j = 0; j < kConvRun; ++j) {
-        const int t = t0 + j;
-        if (t >= a.T) break;
-        conv_in<T, VW, false>(a, b, t, len, c, n, x[K - 1]);
-        float o[VW];
+        for (int j = 0; j < NB; ++j) raw_get(raw[j], a.x, c, x[K - 1 + j]);
+        if (j0 + NB < RUN) load(j0 + NB);
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-            float p = bias[i];
+        for (int j = 0; j < NB; ++j) {
+            float o[VW];
 #pragma unroll
-            for (int k = 0; k < K; ++k) p = fmaf(w[k][i], x[k][i], p);
-            if (a.silu) p *= sigmoid(p);
-            o[i] = t < len ? p : 0.0f;
+            for (int i = 0; i < VW; ++i) {
+                o[i] = bias[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) o[i] = fmaf(w[k][i], x[j + k][i], o[i]);
+            }
+            if (a.silu)
+#pragma unroll
+                for (int i = 0; i < VW; ++i) o[i] *= sigmoid(o[i]);
+            const int t = t0 + j0 + j;
+#pragma unroll
+            for (int i = 0; i < VW; ++i) o[i] = t < len ? o[i] : 0.0f;
+            if (t < t_end) py.store(a.y, j0 + j, n, o);
         }
-        store_vec<T, VW>(a.y, b, t, c, n, o);
 #pragma unroll
         for (int k = 0; k < K - 1; ++k)
 #pragma unroll
-            for (int i = 0; i < VW; ++i) x[k][i] = x[k + 1][i];
+            for (int i = 0; i < VW; ++i) x[k][i] = x[NB + k][i];
     }
 }
 
@@ -94,17 +118,16 @@ __global__ void __launch_bounds__(256) conv_state_kernel(ConvArgs a) {
     reinterpret_cast<T*>(a.state_out)[i] = v;
 }
 
-template <class T, int K>
-__global__ void __launch_bounds__(kConvLanes * kConvRows) conv_backward_kernel(ConvArgs a) {
-    constexpr int VW = conv_vw<K>();
-    __shared__ float part[kConvRows][kConvLanes * VW + 1];
-    const int lane = threadIdx.x % kConvLanes, row = threadIdx.x / kConvLanes;
-    const int c = (blockIdx.x * kConvLanes + lane) * VW, n = a.channels - c;
+template <class T, int K, bool PK>
+__global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(ConvArgs a) {
+    constexpr int VW = kConvVW, NB = conv_batch<K>(), RUN = conv_run<K>(true);
+    __shared__ __align__(16) float part[kConvThreads * VW];      // [rows][lanes * VW]
+    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * VW, n = a.channels - c;
     const int b = blockIdx.z;
-    const int t0 = (blockIdx.y * kConvRows + row) * kConvRun;
+    const int t0 = (blockIdx.y * blockDim.y + threadIdx.y) * RUN;
     const int len = clamp_len(a.lengths, b, a.T);
-    // g[k]: dy act'(pre) of steps t - (K - 1) + k
-    float w[K][VW], dw[K][VW], x[K][VW], g[K][VW], bias[VW], db[VW];
+    // g[j]: dy act'(pre) of the step of x[j]
+    float w[K][VW], dw[K][VW], x[K - 1 + NB][VW], g[K - 1 + NB][VW], bias[VW], db[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
         bias[i] = a.bias && i < n ? a.bias[c + i] : 0.0f;
@@ -112,48 +135,70 @@ __global__ void __launch_bounds__(kConvLanes * kConvRows) conv_backward_kernel(C
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             w[k][i] = i < n ? a.w[(long long)(c + i) * K + k] : 0.0f;
-            dw[k][i] = x[k][i] = g[k][i] = 0.0f;
+            dw[k][i] = 0.0f;
         }
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) g[k][i] = 0.0f;
     }
     if (n > 0 && t0 < a.T) {
+        const int t_end = min(a.T, t0 + RUN);
+        RowIn<T, VW, PK> px;
+        RowIn<T, VW, false> pd;
+        RowOut<T, VW> po;
+        px.init(a.x, b, t0, a.T, c);
+        pd.init(a.dy, b, t0, a.T, c);
+        po.init(a.dx, b, t0, c);
+        Raw<T, VW, PK> rx[NB];
+        Raw<T, VW, false> rd[NB];
+        auto load = [&](int j0) {
 #pragma unroll
-        for (int k = 0; k < K - 1; ++k) conv_in<T, VW, true>(a, b, t0 - (K - 1) + k, len, c, n, x[k]);
-        const int t_end = min(a.T, t0 + kConvRun);
-        for (int t = t0; t < t_end + K - 1; ++t) {
-            // past the run the outputs only give their share of its dx
-            conv_in<T, VW, true>(a, b, t, t < a.T ? len : 0, c, n, x[K - 1]);
-            float dy[VW];
-            Raw<T, VW, false> r;
-            raw_load(r, a.dy, b, t, a.T, c, t < len ? n : 0);
-            raw_get(r, a.dy, c, dy);
+            for (int j = 0; j < NB; ++j) {
+                const int in = t0 + j0 + j < len ? n : 0;
+                px.load(rx[j], a.x, j0 + j, c, in);
+                pd.load(rd[j], a.dy, j0 + j, c, in);
+            }
+        };
+        load(0);
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                float d = dy[i];
-                if (a.silu) {
-                    float p = bias[i], y, ds;
+        for (int k = 0; k < K - 1; ++k) conv_in<T, VW, PK>(a, b, t0 - (K - 1) + k, len, c, n, x[k]);
+        // past the run the outputs only give their share of its dx
+#pragma unroll 1
+        for (int j0 = 0; t0 + j0 < t_end + K - 1; j0 += NB) {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) p = fmaf(w[k][i], x[k][i], p);
-                    dsilu(p, y, ds);
-                    d *= ds;
-                }
-                d = t < len ? d : 0.0f;
-                g[K - 1][i] = d;
-                if (t < t_end) {
+            for (int j = 0; j < NB; ++j) {
+                raw_get(rx[j], a.x, c, x[K - 1 + j]);
+                raw_get(rd[j], a.dy, c, g[K - 1 + j]);
+            }
+            if (j0 + NB < RUN + K - 1) load(j0 + NB);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                if (a.silu)
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) {
+                        float p = bias[i], y, ds;
+#pragma unroll
+                        for (int k = 0; k < K; ++k) p = fmaf(w[k][i], x[j + k][i], p);
+                        dsilu(p, y, ds);
+                        g[K - 1 + j][i] *= ds;
+                    }
+                const int t = t0 + j0 + j;
+                const bool mine = t < t_end;
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    const float d = mine ? g[K - 1 + j][i] : 0.0f;
                     db[i] += d;
 #pragma unroll
-                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(d, x[k][i], dw[k][i]);
+                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(d, x[j + k][i], dw[k][i]);
                 }
-            }
-            // x[s] was read by outputs s .. s + K - 1: output s + j with tap K - 1 - j
-            const int s = t - (K - 1);
-            if (s >= t0) {
+                // x[s] was read by outputs s .. s + K - 1: output s + m with tap K - 1 - m
+                const int s = t - (K - 1);
+                if (s < t0 || s >= t_end) continue;
                 float o[VW];
 #pragma unroll
                 for (int i = 0; i < VW; ++i) {
-                    float v = 0.0f;
+                    o[i] = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < K; ++j) v = fmaf(w[K - 1 - j][i], g[j][i], v);
-                    o[i] = v;
+                    for (int m = 0; m < K; ++m) o[i] = fmaf(w[K - 1 - m][i], g[j + m][i], o[i]);
                 }
                 if (a.dstate_out && s < len) {
                     // x[s] is entry s - (len - (K - 1)) of the state after the last step
@@ -167,26 +212,25 @@ __global__ void __launch_bounds__(kConvLanes * kConvRows) conv_backward_kernel(C
                 }
 #pragma unroll
                 for (int i = 0; i < VW; ++i) o[i] = s < len ? o[i] : 0.0f;
-                store_vec<T, VW>(a.dx, b, s, c, n, o);
+                po.store(a.dx, s - t0, n, o);
             }
 #pragma unroll
             for (int k = 0; k < K - 1; ++k)
 #pragma unroll
-                for (int i = 0; i < VW; ++i) x[k][i] = x[k + 1][i], g[k][i] = g[k + 1][i];
+                for (int i = 0; i < VW; ++i) x[k][i] = x[NB + k][i], g[k][i] = g[NB + k][i];
         }
     }
     // the workgroup's share of dw and dbias: its runs in order
+    const int lanes = blockDim.x * VW, tid = threadIdx.y * blockDim.x + threadIdx.x;
 #pragma unroll
     for (int k = 0; k <= K; ++k) {
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < VW; ++i) part[row][lane * VW + i] = k < K ? dw[k < K ? k : 0][i] : db[i];
+        lds_put(&part[threadIdx.y * lanes + threadIdx.x * VW], k < K ? dw[k < K ? k : 0] : db);
         __syncthreads();
-        if (threadIdx.x < kConvLanes * VW) {
-            const int cc = blockIdx.x * kConvLanes * VW + threadIdx.x;
+        if (tid < lanes) {
+            const int cc = blockIdx.x * lanes + tid;
             float v = 0.0f;
-#pragma unroll
-            for (int r = 0; r < kConvRows; ++r) v += part[r][threadIdx.x];
+            for (int r = 0; r < (int)blockDim.y; ++r) v += part[r * lanes + tid];
             if (cc < a.channels)
                 a.part[(((long long)b * a.tiles + blockIdx.y) * (K + 1) + k) * a.channels + cc] = v;
         }
@@ -274,12 +318,16 @@ __global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {
 
 template <class T, int K>
 hipError_t conv_pass(const ConvArgs& a, bool back, hipStream_t s) {
-    constexpr int VW = conv_vw<K>();
-    const dim3 grid((a.channels + kConvLanes * VW - 1) / (kConvLanes * VW), a.tiles, a.batch);
-    if (back)
-        conv_backward_kernel<T, K><<<grid, kConvLanes * kConvRows, 0, s>>>(a);
+    const int lanes = conv_lanes(a.channels), rows = kConvThreads / lanes;
+    const int runs = (a.T + conv_run(K, back) - 1) / conv_run(K, back);
+    const dim3 block(lanes, rows);
+    const dim3 grid((a.channels + lanes * kConvVW - 1) / (lanes * kConvVW), (runs + rows - 1) / rows, a.batch);
+    if (!back)
+        conv_forward_kernel<T, K><<<grid, block, 0, s>>>(a);
+    else if (a.x.packed)
+        conv_backward_kernel<T, K, true><<<grid, block, 0, s>>>(a);
     else
-        conv_forward_kernel<T, K><<<grid, kConvLanes * kConvRows, 0, s>>>(a);
+        conv_backward_kernel<T, K, false><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -301,7 +349,10 @@ unsigned blocks(long long n) { return (unsigned)((n + 255) / 256); }
 
 }  // namespace
 
-int conv_tiles(int T) { return (T + kConvRun * kConvRows - 1) / (kConvRun * kConvRows); }
+int conv_tiles(int T, int channels, int taps) {
+    const int rows = kConvThreads / conv_lanes(channels), steps = rows * conv_run(taps, true);
+    return (T + steps - 1) / steps;
+}
 
 hipError_t launch_conv_forward(const ConvArgs& a, int dtype, hipStream_t s) {
     SEQ_BY_TYPE(dtype, T, {

@@ -88,7 +88,7 @@ inline int scan_np(int state) { return state <= 4 ? 4 : state <= 8 ? 8 : state <
 inline int scan_cb(int np) { return np <= 16 ? 64 : np == 32 ? 32 : 16; }
 
 // time tiles of the convolution's backward (one share of dw each)
-int conv_tiles(int T);
+int conv_tiles(int T, int channels, int taps);
 
 hipError_t launch_scan_forward(const ScanArgs& a, int dtype, hipStream_t s);
 hipError_t launch_scan_states(const ScanArgs& a, int dtype, hipStream_t s);   // only a.saved
