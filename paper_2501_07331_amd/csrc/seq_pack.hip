@@ -79,11 +79,16 @@ __global__ void __launch_bounds__(256) unpack_kernel(PackArgs a) {
     store_vec<T, 8>(a.x, bt / a.T, bt % a.T, c, a.n - c, x);
 }
 
-// First event of [lo, hi) whose step is not below s.
+// First event of [lo, hi) whose step is not below s: 64 candidates a round.
 __device__ __forceinline__ long long first_at(const int* step, long long lo, long long hi, int s) {
+    const int lane = threadIdx.x % 64;
     while (lo < hi) {
-        const long long mid = lo + (hi - lo) / 2;
-        if (step[mid] < s) lo = mid + 1; else hi = mid;
+        const long long stride = (hi - lo) / 64 + 1, k = lo + lane * stride;
+        const unsigned long long in = __ballot(k < hi), yes = __ballot(k < hi && step[k < hi ? k : lo] >= s);
+        // the answer lies after the last candidate that says no, up to the first that says yes
+        const int first = yes ? __ffsll(yes) - 1 : __popcll(in);
+        if (yes) hi = lo + first * stride;
+        if (first) lo += (first - 1) * stride + 1;
     }
     return lo;
 }
@@ -93,11 +98,13 @@ __device__ __forceinline__ long long first_at(const int* step, long long lo, lon
 // kept below 65536 by the host), and writes them out as vectors.
 template <class T>
 __global__ void __launch_bounds__(256) bin_kernel(BinArgs a) {
-    extern __shared__ unsigned cnt[];
+    extern __shared__ __align__(16) unsigned cnt[];
     __shared__ long long range[2];
     const int b = blockIdx.y, r0 = blockIdx.x * a.tile, nr = min(a.tile, a.rows - r0);
-    const int words = (a.tile * a.n + 1) / 2;
-    if (threadIdx.x < 2) {
+    const int vecs = (a.n + 7) / 8, stride = 8 * vecs;      // counts of a row: whole 16-byte vectors
+    if (threadIdx.x < 128) {
+        // the first wave finds the rows' first event, the second their end
+        const int which = threadIdx.x / 64;
         long long lo, hi;
         if (a.offsets) {
             lo = min(max(a.offsets[b], 0), a.nnz);
@@ -106,28 +113,30 @@ __global__ void __launch_bounds__(256) bin_kernel(BinArgs a) {
             lo = (long long)b * a.capacity;
             hi = lo + min(max(a.count[b], 0), a.capacity);
         }
-        const long long s = (long long)(r0 + (threadIdx.x ? nr : 0)) * a.factor;
-        range[threadIdx.x] = s >= a.T ? hi : first_at(a.step, lo, hi, (int)s);
+        const long long s = (long long)(r0 + (which ? nr : 0)) * a.factor;
+        const long long at = s >= a.T ? hi : first_at(a.step, lo, hi, (int)s);
+        if (threadIdx.x % 64 == 0) range[which] = at;
     }
-    for (int i = threadIdx.x; i < words; i += 256) cnt[i] = 0;
+    uint4* clear = reinterpret_cast<uint4*>(cnt);
+    for (int i = threadIdx.x; i < nr * vecs; i += 256) clear[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     for (long long i = range[0] + threadIdx.x; i < range[1]; i += 256) {
         const int s = a.step[i], c = a.neuron[i];
         const int r = s / a.factor - r0;
         if (s >= 0 && s < a.T && r >= 0 && r < nr && c >= 0 && c < a.n) {
-            const int at = r * a.n + c;
+            const int at = r * stride + c;
             atomicAdd(&cnt[at / 2], 1u << (16 * (at % 2)));
         }
     }
     __syncthreads();
-    const unsigned short* half = reinterpret_cast<const unsigned short*>(cnt);
-    const int vecs = (a.n + 7) / 8;
     for (int i = threadIdx.x; i < nr * vecs; i += 256) {
-        const int r = i / vecs, c = i % vecs * 8, n = a.n - c;
+        const int r = i / vecs, c = i % vecs * 8;
+        const uint4 v = clear[i];
+        const unsigned w[4] = {v.x, v.y, v.z, v.w};
         float o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = j < n ? (float)half[r * a.n + c + j] : 0.0f;
-        store_vec<T, 8>(a.y, b, r0 + r, c, n, o);
+        for (int j = 0; j < 8; ++j) o[j] = (float)(w[j / 2] >> (16 * (j % 2)) & 0xffffu);
+        store_vec<T, 8>(a.y, b, r0 + r, c, a.n - c, o);
     }
 }
 
@@ -151,7 +160,7 @@ hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t s) {
 
 hipError_t launch_bin(const BinArgs& a, int dtype, hipStream_t s) {
     const dim3 grid((a.rows + a.tile - 1) / a.tile, a.batch);
-    const size_t lds = ((size_t)a.tile * a.n + 1) / 2 * 4;
+    const size_t lds = (size_t)a.tile * ((a.n + 7) / 8) * 16;
     SEQ_BY_TYPE(dtype, T, {
         bin_kernel<T><<<grid, 256, lds, s>>>(a);
         return hipGetLastError();
