@@ -55,7 +55,7 @@ struct snn_seq {
     float *carry, *dsum;               // states between the parts of the time axis
     float *bcpart, *apart, *dpart;     // shares of the scan's gradients
     float* cpart;                      // shares of the convolution's; the scan's memory
-    float* states;                     // the scan's states, computed again
+    float *states, *hcarry, *csum;     // the scan's states, computed again
     char err[512];
 };
 
@@ -207,8 +207,11 @@ extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
     const size_t n_bc = train ? (size_t)o->batch * o->T * o->groups * gblocks * 2 * np : 0;
     const size_t n_conv = train ? (size_t)o->batch * conv_tiles(o->T, o->channels, o->taps) * (o->taps + 1) * C : 0;
     auto round4 = [](size_t x) { return (x + 3) & ~(size_t)3; };
-    const size_t n_states = o->flags & SNN_SEQ_RECOMPUTE ? (size_t)o->batch * s->segs * C * np : 0;
-    const size_t n_scan = round4(n_carry) + round4(n_dsum) + round4(n_a) + round4(n_d) + round4(n_bc) + n_states;
+    const bool again = o->flags & SNN_SEQ_RECOMPUTE, parts_again = again && s->bparts > 1;
+    const size_t n_csum = (size_t)o->batch * s->segs * C, n_states = again ? n_csum * np : 0;
+    const size_t n_hcarry = parts_again ? (size_t)o->batch * s->bparts * C * np : 0;
+    const size_t n_scan = round4(n_carry) + round4(n_dsum) + round4(n_a) + round4(n_d) + round4(n_bc) + n_states +
+                          n_hcarry + (parts_again ? n_csum : 0);
     const size_t total = std::max(n_scan, n_conv) * sizeof(float);
     if (total) {
         e = hipMalloc(reinterpret_cast<void**>(&s->mem), total);
@@ -224,7 +227,9 @@ extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
         s->apart = p, p += round4(n_a);
         s->dpart = p, p += round4(n_d);
         s->bcpart = p, p += round4(n_bc);
-        s->states = p;
+        s->states = p, p += n_states;
+        s->hcarry = parts_again ? p : nullptr, p += n_hcarry;
+        s->csum = p;
     }
     *out = s;
     return SNN_OK;
@@ -500,11 +505,12 @@ extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
     a.dh0 = c->dh0;
     a.lengths = c->lengths;
     a.softplus = c->softplus != 0;
+    scan_sizes(s, true, &a);
     if (!c->saved) {
-        scan_sizes(s, false, &a);
+        a.hcarry = s->hcarry;
+        a.csum = s->csum;
         SEQ_TRY(s, launch_scan_states(a, type, s->stream));
     }
-    scan_sizes(s, true, &a);
     SEQ_TRY(s, launch_scan_backward(a, type, s->stream));
     return SNN_OK;
 }

@@ -38,6 +38,10 @@ struct ScanArgs {
     int segs;                              // saved states a sample
     float* carry;                          // [batch][chunks][channels][NP] states / adjoints between parts
     float* dsum;                           // [batch][chunks][channels] sums of delta' of a part
+    // backward pass that computes the states again, in parts: their first states, and the sums of
+    // delta' from a part's start to each saved state; NULL otherwise
+    float* hcarry;                         // [batch][chunks][channels][NP]
+    float* csum;                           // [batch][segs][channels]
     // backward
     const float* dhT;
     float* dh0;

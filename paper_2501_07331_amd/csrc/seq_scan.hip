@@ -11,22 +11,27 @@
 
 namespace {
 
-// What a launch is for: the whole scan; only the saved states (they are
-// computed again for the backward pass); only a part's last state from zero
-// and the sum of its delta', for the join of the parts.
-enum { SCAN_ALL, SCAN_SAVE, SCAN_ENDS };
+// What a launch is for: the whole scan; only a part's last state from zero and
+// the sum of its delta', for the join of the parts; and for a backward pass
+// that computes the states again, the saved states of an undivided time axis
+// (SAVE), or of its parts, each from zero, with the sums of delta' up to them
+// and, in the same pass, the parts' adjoints at their starts (BOTH).
+enum { SCAN_ALL, SCAN_SAVE, SCAN_ENDS, SCAN_BOTH };
 
 // One part of the time axis of CB channels.
 template <class T, int S, int MODE>
 __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs a) {
     constexpr int NP = ScanShape<S>::NP, CB = ScanShape<S>::CB, NT = ScanShape<S>::NT, TT = kScanTile;
-    constexpr bool STATES = MODE != SCAN_ALL, ENDS = MODE == SCAN_ENDS;
+    constexpr bool BOTH = MODE == SCAN_BOTH, STATES = MODE != SCAN_ALL, ENDS = MODE == SCAN_ENDS || BOTH;
+    constexpr bool WITH_C = !STATES || BOTH;
+    constexpr int BW = WITH_C ? 2 * NP : NP;
     constexpr int EP = TT * CB / NT;              // elements a thread
     constexpr int VW = EP < 8 ? EP : 8, NV = EP / VW, VR = CB / VW, PR = NT / VR;
     __shared__ __align__(16) float2 ds[TT][CB];   // (delta', delta' u)
     // sum_n C h; four steps are written at once, which the padding puts on different banks
     __shared__ __align__(16) float yl[STATES ? 1 : TT][CB + 16];
-    __shared__ __align__(16) float bc[TT * (STATES ? NP : 2 * NP)];
+    __shared__ __align__(16) float dyl[BOTH ? TT : 1][CB];   // dy'
+    __shared__ __align__(16) float bc[TT * BW];
 
     const int tid = threadIdx.x;
     const int blk = blockIdx.x % (a.groups * a.gblocks), b = blockIdx.x / (a.groups * a.gblocks), part = blockIdx.y;
@@ -37,7 +42,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
 
     // elementwise role: VW channels from ecol of the rows erow, erow + PR, ...
     const int ecol = (tid % VR) * VW, erow = tid / VR, en = nc - ecol;
-    const bool gated = !STATES && a.z.p;
+    const bool gated = WITH_C && a.z.p;
     float bias[VW], Dv[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
@@ -49,6 +54,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
     const bool live = ch < nc;
     const long long cidx = (long long)b * a.channels + c0 + ch;
     float A2[4], h[4], dsum = 0.0f;
+    float decay[4] = {1.0f, 1.0f, 1.0f, 1.0f}, gr[4] = {};   // BOTH: from the part's start; its adjoint there
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int n = 4 * q + k;
@@ -72,7 +78,10 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
     pd.init(a.delta, b, erow, a.T, c0 + ecol);
     if (gated) pz.init(a.z, b, erow, a.T, c0 + ecol);
     if (!STATES) py.init(a.y, b, erow, c0 + ecol);
-    GroupTile<T, S, TT, !STATES> gt;
+    Raw<T, VW, false> ry[NV];
+    RowIn<T, VW, false> pdy;
+    if (BOTH) pdy.init(a.dy, b, erow, a.T, c0 + ecol);
+    GroupTile<T, S, TT, WITH_C> gt;
     gt.init(a, b, g, tid);
     auto load = [&](int t0) {
 #pragma unroll
@@ -82,6 +91,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
             pu.load(ru[v], a.u, t0 + v * PR, c0 + ecol, n);
             pd.load(rd[v], a.delta, t0 + v * PR, c0 + ecol, n);
             if (gated) pz.load(rz[v], a.z, t0 + v * PR, c0 + ecol, n);
+            if (BOTH) pdy.load(ry[v], a.dy, t0 + v * PR, c0 + ecol, n);
         }
         gt.load(a, t0, min(len, t_end), tid);
     };
@@ -115,31 +125,48 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
 #pragma unroll
                 for (int i = 0; i < VW; ++i) gate[v][i] *= sigmoid(gate[v][i]);
             }
+            if constexpr (BOTH) {
+                float dy[VW];
+                raw_get(ry[v], a.dy, c0 + ecol, dy);
+                if (gated)
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) dy[i] *= gate[v][i];
+                lds_put(&dyl[r][ecol], dy);
+            }
         }
         gt.store(bc, tid);
         __syncthreads();
         if (t0 + TT < t_end) load(t0 + TT);
 
         for (int r8 = 0; r8 < nv; r8 += 8) {
-            if (!ENDS && a.saved && r8 % kScanSeg == 0 && live)
-                *reinterpret_cast<float4*>(
-                    a.saved + (((long long)b * a.segs + (t0 + r8) / kScanSeg) * a.channels + c0 + ch) * NP + 4 * q) =
-                    make_float4(h[0], h[1], h[2], h[3]);
+            if (MODE != SCAN_ENDS && a.saved && r8 % kScanSeg == 0 && live) {
+                const long long at = ((long long)b * a.segs + (t0 + r8) / kScanSeg) * a.channels + c0 + ch;
+                *reinterpret_cast<float4*>(a.saved + at * NP + 4 * q) = make_float4(h[0], h[1], h[2], h[3]);
+                if (BOTH && q == 0) a.csum[at] = dsum;
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int r = r8 + j;
                 const float2 d = ds[r][ch];
-                float4 Bv, Cv;
-                if constexpr (STATES) {
-                    Bv = *reinterpret_cast<const float4*>(&bc[r * NP + 4 * q]);
-                } else {
-                    Bv = *reinterpret_cast<const float4*>(&bc[r * 2 * NP + 4 * q]);
-                    Cv = *reinterpret_cast<const float4*>(&bc[r * 2 * NP + NP + 4 * q]);
+                const float4 Bv = *reinterpret_cast<const float4*>(&bc[r * BW + 4 * q]);
+                float4 Cv;
+                if constexpr (WITH_C) Cv = *reinterpret_cast<const float4*>(&bc[r * BW + NP + 4 * q]);
+                const float Bk[4] = {Bv.x, Bv.y, Bv.z, Bv.w};
+                float e[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    e[k] = exp2_fast(d.x * A2[k]);
+                    h[k] = fmaf(e[k], h[k], d.y * Bk[k]);
                 }
-                h[0] = fmaf(exp2_fast(d.x * A2[0]), h[0], d.y * Bv.x);
-                h[1] = fmaf(exp2_fast(d.x * A2[1]), h[1], d.y * Bv.y);
-                h[2] = fmaf(exp2_fast(d.x * A2[2]), h[2], d.y * Bv.z);
-                h[3] = fmaf(exp2_fast(d.x * A2[3]), h[3], d.y * Bv.w);
+                if constexpr (BOTH) {
+                    const float dyp = dyl[r][ch];
+                    const float Ck[4] = {Cv.x, Cv.y, Cv.z, Cv.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        decay[k] *= e[k];
+                        gr[k] = fmaf(decay[k] * Ck[k], dyp, gr[k]);
+                    }
+                }
                 if constexpr (ENDS) dsum += d.x;
                 if constexpr (!STATES) {
                     float y = Cv.x * h[0];
@@ -176,7 +203,8 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
     if (!live) return;
     if constexpr (ENDS) {
         const long long at = ((long long)b * a.chunks + part) * a.channels + c0 + ch;
-        *reinterpret_cast<float4*>(a.carry + at * NP + 4 * q) = make_float4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<float4*>((BOTH ? a.hcarry : a.carry) + at * NP + 4 * q) = make_float4(h[0], h[1], h[2], h[3]);
+        if (BOTH) *reinterpret_cast<float4*>(a.carry + at * NP + 4 * q) = make_float4(gr[0], gr[1], gr[2], gr[3]);
         if (q == 0) a.dsum[at] = dsum;
     } else if (!STATES && part == a.chunks - 1 && a.hT) {
 #pragma unroll
@@ -187,7 +215,7 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
 
 // The states that the parts start from, in the place of those that they end
 // in from zero: H[0] = h0, H[k + 1] = exp(A sum delta') H[k] + end[k].
-__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, int NP) {
+__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, float* carry, int NP) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long per = (long long)a.channels * NP;
     if (i >= a.batch * per) return;
@@ -204,17 +232,22 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, int NP) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool some = k + j + 1 < a.chunks;
-            end[j] = some ? a.carry[(at + j * step) * NP + n] : 0.0f;
+            end[j] = some ? carry[(at + j * step) * NP + n] : 0.0f;
             sum[j] = some ? a.dsum[at + j * step] : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (k + j >= a.chunks) break;
-            a.carry[(at + j * step) * NP + n] = h;
+            carry[(at + j * step) * NP + n] = h;
             h = fmaf(exp2_fast(sum[j] * A2), h, end[j]);
         }
         at += 8 * step;
     }
+}
+
+void join_states(const ScanArgs& a, float* carry, int NP, hipStream_t s) {
+    const long long n = (long long)a.batch * a.channels * NP;
+    scan_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, carry, NP);
 }
 
 // One step: a lane holds four states of a channel, S lanes a channel.
@@ -270,27 +303,28 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
     }
 }
 
-template <class T, int S, int MODE>
-hipError_t run(const ScanArgs& a, hipStream_t s) {
+template <class T, int S>
+hipError_t forward(const ScanArgs& a, hipStream_t s) {
     const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
     if (a.chunks > 1) {
         // the last part's end is nobody's start
         scan_forward_kernel<T, S, SCAN_ENDS><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
-        const long long n = (long long)a.batch * a.channels * ScanShape<S>::NP;
-        scan_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, ScanShape<S>::NP);
+        join_states(a, a.carry, ScanShape<S>::NP, s);
     }
-    scan_forward_kernel<T, S, MODE><<<grid, block, 0, s>>>(a);
+    scan_forward_kernel<T, S, SCAN_ALL><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <class T, int S>
-hipError_t forward(const ScanArgs& a, hipStream_t s) {
-    return run<T, S, SCAN_ALL>(a, s);
-}
-
-template <class T, int S>
 hipError_t states(const ScanArgs& a, hipStream_t s) {
-    return run<T, S, SCAN_SAVE>(a, s);
+    const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
+    if (a.chunks > 1) {
+        scan_forward_kernel<T, S, SCAN_BOTH><<<grid, block, 0, s>>>(a);
+        join_states(a, a.hcarry, ScanShape<S>::NP, s);
+    } else {
+        scan_forward_kernel<T, S, SCAN_SAVE><<<grid, block, 0, s>>>(a);
+    }
+    return hipGetLastError();
 }
 
 template <class T, int S>

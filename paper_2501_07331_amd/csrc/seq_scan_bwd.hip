@@ -97,6 +97,15 @@ scan_backward_kernel(ScanArgs a) {
         gr[0] = v.x, gr[1] = v.y, gr[2] = v.z, gr[3] = v.w;
     }
 
+    // the part's first state, where the saved ones were computed again from zero
+    float hp[4] = {}, cs = 0.0f;
+    const bool local = !STATES && a.hcarry;
+    if (local && live) {
+        const float4 v = *reinterpret_cast<const float4*>(
+            a.hcarry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
+        hp[0] = v.x, hp[1] = v.y, hp[2] = v.z, hp[3] = v.w;
+    }
+
     constexpr int R = S < 4 ? S : 4, M = 16 / S < 4 ? 16 / S : 4;
     float* bcout = STATES ? nullptr
                           : a.bcpart + (((long long)b * a.T + tid * SV / BW) * nblk + blk) * BW + tid * SV % BW;
@@ -125,9 +134,11 @@ scan_backward_kernel(ScanArgs a) {
     auto load = [&](int t0) {
         h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (t0 >= len) return;
-        if (!STATES && live)
-            h4 = *reinterpret_cast<const float4*>(
-                a.saved + (((long long)b * a.segs + t0 / TT) * a.channels + c0 + ch) * NP + 4 * q);
+        if (!STATES && live) {
+            const long long at = ((long long)b * a.segs + t0 / TT) * a.channels + c0 + ch;
+            h4 = *reinterpret_cast<const float4*>(a.saved + at * NP + 4 * q);
+            if (local) cs = a.csum[at];
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int t = t0 + erow + v * PR, n = t < len && t < t_end ? en : 0;
@@ -198,7 +209,13 @@ scan_backward_kernel(ScanArgs a) {
             lds_put(&dyl[r][ecol], dy);
         }
         gt.store(bc, tid);
-        const float4 hs = h4;
+        float4 hs = h4;
+        if (local) {
+            hs.x = fmaf(exp2_fast(cs * A2[0]), hp[0], hs.x);
+            hs.y = fmaf(exp2_fast(cs * A2[1]), hp[1], hs.y);
+            hs.z = fmaf(exp2_fast(cs * A2[2]), hp[2], hs.z);
+            hs.w = fmaf(exp2_fast(cs * A2[3]), hp[3], hs.w);
+        }
         __syncthreads();
         if (t0 > t_begin) load(t0 - TT);
 
@@ -454,7 +471,8 @@ hipError_t passes(const ScanArgs& a, hipStream_t s) {
     const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
     if (a.chunks > 1) {
         // the first part's start is nobody's end
-        scan_backward_kernel<T, S, true, PK><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
+        // (computed with the states where these are computed again)
+        if (!a.hcarry) scan_backward_kernel<T, S, true, PK><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
         const long long n = (long long)a.batch * a.channels * NP;
         scan_join_back_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, NP);
     }
