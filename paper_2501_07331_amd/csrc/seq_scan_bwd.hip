@@ -15,8 +15,6 @@
 
 namespace {
 
-constexpr int kAhead = 4;
-
 __device__ __forceinline__ void swap_add32(float& a, float b) {
     // lower lanes: a of both halves, upper lanes: b of both halves
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
@@ -255,8 +253,6 @@ scan_backward_kernel(ScanArgs a) {
                 // each of the channel's lanes keeps one of R steps, for one store
                 k0 = r % R == 0 || q == r % R ? y : k0;
                 if (r % R == R - 1 && (S <= R || q < R)) yl[r - (R - 1) + q][ch] = k0;
-                // reads of LDS run ahead of their use by at most kAhead steps, for the registers' sake
-                if (r % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
             }
             // B and delta' are read again: kept from above they would fill the registers
             asm volatile("" ::: "memory");
@@ -296,12 +292,10 @@ scan_backward_kernel(ScanArgs a) {
                 m1 = r % M == M - 1 || copy == r % M ? dB[1] : m1;
                 if (r % M == 0 && (16 / S <= M || copy < M))
                     *reinterpret_cast<float2*>(&red[r + copy][wave * BW + at]) = make_float2(m0, m1);
-                if (r % kAhead == 0) {
-                    // dA's sums stay here: put off, they would keep 64 products alive
+                // dA's sums stay here: put off, they would keep the tile's products alive
+                if (r % 4 == 0)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(dA[k]));
-                    __builtin_amdgcn_sched_barrier(0);
-                }
             }
         }
         __syncthreads();
