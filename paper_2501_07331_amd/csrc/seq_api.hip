@@ -34,6 +34,12 @@ struct OnDevice {
 // 900) 156 us whole and 138 divided, 1680 waves (28 x 500 x 900) 104 whole and
 // 128 divided; forward and backward, 1680 waves, 382 with a whole backward
 // and 451 with a divided one.  len: steps a part, whole tiles.
+// Up to kJoinParts parts are joined by the workgroups that start them, each for
+// itself; more of them by a launch of their own, once.  At 5 x 333 x 150 (11
+// parts) a training pass takes 57 us with the launch and 53 without, at 16 x
+// 400 x 512 (4 parts) 141 and 131, at 1 x 16384 x 1024 (64 parts) the forward
+// 165 and 160.
+constexpr int kJoinParts = 64;
 constexpr int kFwdWaves = 1408, kBwdWaves = 1024, kFwdFill = 4, kBwdFill = 2;
 void time_parts(int T, long long waves, int enough, int fill, int* parts, int* len) {
     const long long want = waves >= enough ? 1 : (1024 * fill + waves - 1) / waves;
@@ -152,6 +158,7 @@ void scan_sizes(const snn_seq* s, bool back, ScanArgs* k) {
     k->gblocks = s->gblocks;
     k->chunks = back ? s->bparts : s->parts;
     k->chunk_len = back ? s->bpart_len : s->part_len;
+    k->joined = k->chunks > kJoinParts;
     k->segs = s->segs;
     k->carry = s->carry;
     k->dsum = s->dsum;

@@ -35,6 +35,7 @@ struct ScanArgs {
     int per;                               // channels a group
     int gblocks;                           // channel blocks a group
     int chunks, chunk_len;                 // parts of the time axis; steps a part (whole tiles)
+    int joined;                            // a launch of its own joins them
     int segs;                              // saved states a sample
     float* carry;                          // [batch][chunks][channels][NP] states / adjoints between parts
     float* dsum;                           // [batch][chunks][channels] sums of delta' of a part

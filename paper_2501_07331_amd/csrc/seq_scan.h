@@ -50,4 +50,33 @@ struct GroupTile {
     }
 };
 
+// The join of the parts of the time axis, by the workgroup that starts one.
+// carry holds the state (adjoint) at each part's end (start) from zero; h comes
+// in as the first part's start (the last one's end) and goes through the parts
+// before this one:  h = exp(A sum delta') h + end.  at: [b][0][channel];
+// dir: 1 forward, over parts 0 .. n - 1; -1 backward, from the last part down.
+__device__ __forceinline__ void through_parts(const ScanArgs& a, const float* carry, long long at, int np, int q, int dir, int n,
+                                              const float (&A2)[4], float (&h)[4]) {
+    const int first = dir > 0 ? 0 : a.chunks - 1;
+    // four parts' values are loaded before the first is used
+    for (int j = 0; j < n; j += 4) {
+        float4 end[4];
+        float sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long p = at + (long long)(first + dir * (j + i < n ? j + i : j)) * a.channels;
+            end[i] = *reinterpret_cast<const float4*>(carry + p * np + 4 * q);
+            sum[i] = a.dsum[p];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (j + i >= n) break;
+            h[0] = fmaf(exp2_fast(sum[i] * A2[0]), h[0], end[i].x);
+            h[1] = fmaf(exp2_fast(sum[i] * A2[1]), h[1], end[i].y);
+            h[2] = fmaf(exp2_fast(sum[i] * A2[2]), h[2], end[i].z);
+            h[3] = fmaf(exp2_fast(sum[i] * A2[3]), h[3], end[i].w);
+        }
+    }
+}
+
 }  // namespace

@@ -61,12 +61,16 @@ __global__ void __launch_bounds__(ScanShape<S>::NT) scan_forward_kernel(ScanArgs
         const bool in = live && n < a.state;
         A2[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] * kLog2e : 0.0f;
         h[k] = 0.0f;
-        if (!ENDS && in && part == 0 && a.h0) h[k] = a.h0[cidx * a.state + n];
+        if (!ENDS && in && a.h0) h[k] = a.h0[cidx * a.state + n];
     }
     if (!ENDS && live && part > 0) {
-        const float4 v = *reinterpret_cast<const float4*>(
-            a.carry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
-        h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
+        const long long first = (long long)b * a.chunks * a.channels + c0 + ch;
+        if (a.joined) {
+            const float4 v = *reinterpret_cast<const float4*>(a.carry + (first + (long long)part * a.channels) * NP + 4 * q);
+            h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
+        } else {
+            through_parts(a, a.carry, first, NP, q, 1, part, A2, h);
+        }
     }
 
     constexpr int R = S < 4 ? S : 4;
@@ -309,7 +313,7 @@ hipError_t forward(const ScanArgs& a, hipStream_t s) {
     if (a.chunks > 1) {
         // the last part's end is nobody's start
         scan_forward_kernel<T, S, SCAN_ENDS><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
-        join_states(a, a.carry, ScanShape<S>::NP, s);
+        if (a.joined) join_states(a, a.carry, ScanShape<S>::NP, s);
     }
     scan_forward_kernel<T, S, SCAN_ALL><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
@@ -320,7 +324,7 @@ hipError_t states(const ScanArgs& a, hipStream_t s) {
     const dim3 grid(a.batch * a.groups * a.gblocks, a.chunks), block(ScanShape<S>::NT);
     if (a.chunks > 1) {
         scan_forward_kernel<T, S, SCAN_BOTH><<<grid, block, 0, s>>>(a);
-        join_states(a, a.hcarry, ScanShape<S>::NP, s);
+        if (a.joined) join_states(a, a.hcarry, ScanShape<S>::NP, s);
     } else {
         scan_forward_kernel<T, S, SCAN_SAVE><<<grid, block, 0, s>>>(a);
     }

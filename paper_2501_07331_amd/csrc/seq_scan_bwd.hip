@@ -87,21 +87,29 @@ scan_backward_kernel(ScanArgs a) {
         const bool in = live && n < a.state;
         A2[k] = in ? a.A[(long long)(c0 + ch) * a.state + n] * kLog2e : 0.0f;
         dA[k] = gr[k] = 0.0f;
-        if (!STATES && a.chunks == 1 && in && a.dhT) gr[k] = a.dhT[cidx * a.state + n];
+        if (!STATES && in && a.dhT) gr[k] = a.dhT[cidx * a.state + n];
     }
-    if (!STATES && live && a.chunks > 1) {
-        const float4 v = *reinterpret_cast<const float4*>(
-            a.carry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
-        gr[0] = v.x, gr[1] = v.y, gr[2] = v.z, gr[3] = v.w;
-    }
-
-    // the part's first state, where the saved ones were computed again from zero
+    // hp: the part's first state, where the saved ones were computed again from zero
     float hp[4] = {}, cs = 0.0f;
     const bool local = !STATES && a.hcarry;
-    if (local && live) {
-        const float4 v = *reinterpret_cast<const float4*>(
-            a.hcarry + (((long long)b * a.chunks + part) * a.channels + c0 + ch) * NP + 4 * q);
-        hp[0] = v.x, hp[1] = v.y, hp[2] = v.z, hp[3] = v.w;
+    if (!STATES && live && a.chunks > 1) {
+        const long long first = (long long)b * a.chunks * a.channels + c0 + ch;
+        const long long at = (first + (long long)part * a.channels) * NP + 4 * q;
+        if (local)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (a.h0 && 4 * q + k < a.state) hp[k] = a.h0[cidx * a.state + 4 * q + k];
+        if (a.joined) {
+            float4 v = *reinterpret_cast<const float4*>(a.carry + at);
+            gr[0] = v.x, gr[1] = v.y, gr[2] = v.z, gr[3] = v.w;
+            if (local) {
+                v = *reinterpret_cast<const float4*>(a.hcarry + at);
+                hp[0] = v.x, hp[1] = v.y, hp[2] = v.z, hp[3] = v.w;
+            }
+        } else {
+            through_parts(a, a.carry, first, NP, q, -1, a.chunks - 1 - part, A2, gr);
+            if (local) through_parts(a, a.hcarry, first, NP, q, 1, part, A2, hp);
+        }
     }
 
     constexpr int R = S < 4 ? S : 4, M = 16 / S < 4 ? 16 / S : 4;
@@ -468,7 +476,7 @@ hipError_t passes(const ScanArgs& a, hipStream_t s) {
         // (computed with the states where these are computed again)
         if (!a.hcarry) scan_backward_kernel<T, S, true, PK><<<dim3(grid.x, a.chunks - 1), block, 0, s>>>(a);
         const long long n = (long long)a.batch * a.channels * NP;
-        scan_join_back_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, NP);
+        if (a.joined) scan_join_back_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a, NP);
     }
     scan_backward_kernel<T, S, false, PK><<<grid, block, 0, s>>>(a);
     const long long bc = (long long)a.batch * a.T * 2 * a.groups * a.state;
