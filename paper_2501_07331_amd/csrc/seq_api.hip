@@ -267,6 +267,7 @@ static int bin(snn_seq* s, BinArgs& a, int n, int factor, const snn_tensor* dst)
     a.factor = factor;
     a.rows = (s->o.T + factor - 1) / factor;
     ARG(out_arg(s, *dst, "dst", n, a.rows, -1, &a.y));
+    a.past = (size_t)a.batch * a.rows * n * (dst->dtype == SNN_F32 ? 4 : 2) > (32u << 20);
     // rows a workgroup: 16 KiB of counts, so that several workgroups share a CU, or one row
     a.tile = std::min(a.rows, std::max(1, 8192 / n));
     SEQ_TRY(s, launch_bin(a, dst->dtype, s->stream));

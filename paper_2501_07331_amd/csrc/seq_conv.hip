@@ -7,7 +7,8 @@
 // not the width of a load, carries the bandwidth.  The backward pass goes over
 // the same run in the same order: the pre-activation is made again from x, and
 // dx[t] leaves when the last output that read x[t] is done, taps - 1 steps
-// later.
+// later.  At 32 x 1000 x 1024, 4 taps, bf16: forward 40 us (131 MB, 3.3 TB/s),
+// backward 58 us (197 MB, 3.4 TB/s) and 5 us for the sums over workgroups.
 #include "seq_device.h"
 
 namespace {

@@ -114,7 +114,8 @@ __device__ __forceinline__ void raw_get(const Raw<T, N, PK>& r, const SeqT& s, i
     for (int i = 0; i < N; ++i) o[i] = (float)r.e[i];
 }
 
-template <class T, int N>
+// PAST: past the caches, for what is too long to be found there again.
+template <class T, int N, bool PAST = false>
 __device__ __forceinline__ void store_at(T* p, int n, const float (&o)[N]) {
     if (n >= N) {
         if constexpr (N == 1) *p = (T)o[0];
@@ -122,7 +123,8 @@ __device__ __forceinline__ void store_at(T* p, int n, const float (&o)[N]) {
             typename Vec<T, N>::type v;
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = (T)o[i];
-            *reinterpret_cast<typename Vec<T, N>::type*>(p) = v;
+            if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Vec<T, N>::type*>(p));
+            else *reinterpret_cast<typename Vec<T, N>::type*>(p) = v;
         }
     } else {
 #pragma unroll

@@ -85,6 +85,7 @@ struct BinArgs {
     int nnz, capacity;
     SeqT y;
     int batch, T, n, factor, rows, tile;   // rows of the output, rows of a workgroup
+    int past;                              // the output goes past the caches
 };
 
 // states of a channel, padded to what the lanes of a channel hold (4 each)

@@ -3,7 +3,10 @@
 
 namespace {
 
-// Sixteen lanes share a block of 128 channels, 8 each; a wave has four blocks.
+// Bound by memory: a lane takes 8 channels, so that its load is 16 bytes of a
+// 16-bit type and its store 8; sixteen lanes share a block of 128 channels and
+// find its largest value with four DPP steps.  64 x 1000 x 512 in bf16, 98 MB:
+// 19 us packed, 17 us unpacked (5.1 and 5.8 TB/s).
 constexpr int kPackLanes = SNN_SEQ_BLOCK / 8;
 
 __device__ __forceinline__ float row_max(float x) {
@@ -95,7 +98,10 @@ __device__ __forceinline__ long long first_at(const int* step, long long lo, lon
 
 // A workgroup counts `tile` rows of the output in LDS, two 16-bit counts a
 // word (a neuron has at most one spike a step, and factor <= T <= 65536 is
-// kept below 65536 by the host), and writes them out as vectors.
+// kept below 65536 by the host), and writes them out as vectors.  Bound by the
+// output: 256 samples of 700 channels in 250 bins, 90 MB of bf16, take 24 us
+// (4.5 TB/s with the events), 37 us with stores through the caches, which an
+// output beyond their 32 MB only passes through.
 template <class T>
 __global__ void __launch_bounds__(256) bin_kernel(BinArgs a) {
     extern __shared__ __align__(16) unsigned cnt[];
@@ -136,7 +142,9 @@ __global__ void __launch_bounds__(256) bin_kernel(BinArgs a) {
         float o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = (float)(w[j / 2] >> (16 * (j % 2)) & 0xffffu);
-        store_vec<T, 8>(a.y, b, r0 + r, c, a.n - c, o);
+        T* to = reinterpret_cast<T*>(a.y.p) + b * a.y.sample + (r0 + r) * a.y.row + c;
+        if (a.past) store_at<T, 8, true>(to, a.n - c, o);
+        else store_at<T, 8>(to, a.n - c, o);
     }
 }
 
