@@ -65,6 +65,8 @@ def measured_traffic(kernel):
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2501_07331_amd", "csrc")
     for f in sorted(os.listdir(d)):
+        if not f.startswith("snn_"):      # the sequence operators' sources: no part of this step
+            continue
         with open(os.path.join(d, f), "rb") as fh:
             h.update(fh.read())
     if rec.get("source_sha256") != h.hexdigest() or f"traffic {kernel}" not in rec:
