@@ -20,13 +20,13 @@
  *
  * Memory and streams.  Every pointer is device memory of the handle's device
  * (the one current in create), owned by the caller, unless marked (host).
- * Outputs are fully overwritten and must not overlap inputs, except where
- * stated.  A handle owns its scratch, allocated in create; no other call
+ * Outputs are fully overwritten and must not overlap inputs or one another,
+ * except where stated.  A handle owns its scratch, allocated in create; no other call
  * allocates, waits for the device or reads back: a call checks its arguments,
  * enqueues its kernels on the handle's stream and returns, so it can be
  * captured into a graph.  Calls on one handle share its scratch: graphs
  * captured from one handle must not run at the same time as each other or as
- * its calls on another stream.  Distinct handles are independent.  A handle
+ * its calls on another stream, nor after it is destroyed.  Distinct handles are independent.  A handle
  * is not thread-safe.
  *
  * Lengths.  `lengths` [batch] (or NULL: T each) gives the valid steps of each

@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "seq_internal.h"
 #include "seq_sample.h"
@@ -139,6 +140,18 @@ int out_arg(snn_seq* s, const snn_tensor& t, const char* name, int n, int T, int
 int f32_arg(snn_seq* s, const void* p, const char* name, bool need) {
     if (!p && need) return fail(s, SNN_EINVAL, "%s: NULL", name);
     if (reinterpret_cast<uintptr_t>(p) % 4) return fail(s, SNN_EINVAL, "%s: misaligned", name);
+    return SNN_OK;
+}
+
+// No output is an input, nor another output (partial overlaps are the caller's to avoid).
+int distinct(snn_seq* s, std::initializer_list<const void*> in, std::initializer_list<const void*> out) {
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        if (!*o) continue;
+        for (const void* i : in)
+            if (i == *o) return fail(s, SNN_EINVAL, "an output is an input");
+        for (auto p = out.begin(); p != o; ++p)
+            if (*p == *o) return fail(s, SNN_EINVAL, "two outputs are one");
+    }
     return SNN_OK;
 }
 
@@ -363,7 +376,7 @@ extern "C" int snn_seq_conv_forward(snn_seq* s, const snn_seq_conv* c) {
     SEQ_ENTER(s);
     ConvArgs a{};
     ARG(conv_args(s, c, s->o.T, &a));
-    if (a.state_out && a.state_out == a.state) return fail(s, SNN_EINVAL, "state_out is state");
+    ARG(distinct(s, {c->x.data, c->w, c->bias, c->state}, {c->y.data, c->state_out}));
     SEQ_TRY(s, launch_conv_forward(a, c->x.dtype, s->stream));
     return SNN_OK;
 }
@@ -372,6 +385,8 @@ extern "C" int snn_seq_conv_step(snn_seq* s, const snn_seq_conv* c) {
     SEQ_ENTER(s);
     ConvArgs a{};
     ARG(conv_args(s, c, 1, &a));
+    ARG(distinct(s, {c->x.data, c->w, c->bias, c->state}, {c->y.data}));
+    ARG(distinct(s, {c->x.data, c->w, c->bias, c->y.data}, {c->state_out}));
     if (a.lengths) return fail(s, SNN_EINVAL, "lengths: a step has none");
     SEQ_TRY(s, launch_conv_step(a, c->x.dtype, s->stream));
     return SNN_OK;
@@ -406,6 +421,8 @@ extern "C" int snn_seq_conv_backward(snn_seq* s, const snn_seq_conv_grad* c) {
     a.silu = c->silu != 0;
     a.tiles = conv_tiles(T, C, s->o.taps);
     a.part = s->cpart;
+    ARG(distinct(s, {c->x.data, c->x.scale, c->dy.data, c->w, c->bias, c->state, c->dstate_out},
+                 {c->dx.data, c->dw, c->dbias, c->dstate}));
     SEQ_TRY(s, launch_conv_backward(a, type, s->stream));
     return SNN_OK;
 }
@@ -444,7 +461,8 @@ extern "C" int snn_seq_scan_forward(snn_seq* s, const snn_seq_scan* c) {
     SEQ_ENTER(s);
     ScanArgs a{};
     ARG(scan_args(s, c, s->o.T, &a));
-    if (a.hT && a.hT == a.h0) return fail(s, SNN_EINVAL, "hT is h0");
+    ARG(distinct(s, {c->u.data, c->delta.data, c->B.data, c->C.data, c->z.data, c->A, c->D, c->delta_bias, c->h0},
+                 {c->y.data, c->hT, c->saved}));
     SEQ_TRY(s, launch_scan_forward(a, c->u.dtype, s->stream));
     return SNN_OK;
 }
@@ -454,6 +472,10 @@ extern "C" int snn_seq_scan_step(snn_seq* s, const snn_seq_scan* c) {
     ScanArgs a{};
     ARG(scan_args(s, c, 1, &a));
     if (!a.hT) return fail(s, SNN_EINVAL, "hT: NULL");
+    ARG(distinct(s, {c->u.data, c->delta.data, c->B.data, c->C.data, c->z.data, c->A, c->D, c->delta_bias, c->h0},
+                 {c->y.data}));
+    ARG(distinct(s, {c->u.data, c->delta.data, c->B.data, c->C.data, c->z.data, c->A, c->D, c->delta_bias, c->y.data},
+                 {c->hT}));
     if (a.lengths || a.saved) return fail(s, SNN_EINVAL, "lengths, saved: a step has none");
     SEQ_TRY(s, launch_scan_step(a, c->u.dtype, s->stream));
     return SNN_OK;
@@ -513,6 +535,9 @@ extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
     a.dh0 = c->dh0;
     a.lengths = c->lengths;
     a.softplus = c->softplus != 0;
+    ARG(distinct(s, {c->u.data, c->u.scale, c->delta.data, c->delta.scale, c->B.data, c->C.data, c->z.data, c->z.scale,
+                     c->dy.data, c->A, c->D, c->delta_bias, c->h0, c->dhT, c->saved},
+                 {c->du.data, c->ddelta.data, c->dB.data, c->dC.data, c->dz.data, c->dA, c->dD, c->ddelta_bias, c->dh0}));
     scan_sizes(s, true, &a);
     if (!c->saved) {
         a.hcarry = s->hcarry;

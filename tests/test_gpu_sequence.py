@@ -171,6 +171,8 @@ SCAN = [
     (2, 200, 24, 12, 1, "bfloat16", [70, 200], True, True, True),   # a part behind a sample's end
     (1, 130, 3, 33, 1, "float16", None, True, True, True),
     (2, 96, 4, 4, 4, "float32", [64, -1], False, False, False),
+    (1, 2300, 3, 4, 1, "float32", None, True, True, False),         # more parts than their workgroups join themselves
+    (2, 2200, 2, 9, 1, "bfloat16", [2200, 1234], False, True, False),
 ]
 
 
@@ -252,6 +254,72 @@ def test_scan_from_packed_activations(packed, dtype, lengths, C, N, G):
     ref = seq.scan(**v, lengths=lengths, dy=dy, dhT=dhT)
     size = seq.scan(**v, lengths=lengths, dy=dy, dhT=dhT, absolute=True)
     _check_scan(grad, ref, size, B, T, C, G, N, dtype)
+
+
+@pytest.mark.parametrize("N,dtype,recompute", [(16, "bfloat16", False), (16, "float32", True), (8, "float16", True),
+                                               (3, "float32", False), (30, "bfloat16", True)])
+def test_scan_of_a_batch_that_fills_the_chip(N, dtype, recompute):
+    """Enough rows for an undivided time axis, of many tiles: a thousand copies of two samples, whose outputs are
+    theirs and whose parameter gradients are five hundred times their sums."""
+    torch = _torch()
+    B, T, C, copies = 2, 90, 70, 512
+    v, dy, dhT = _scan_inputs(B, T, C, N, 1, dtype, True, True, N)
+    rep = lambda x: np.tile(x, (copies,) + (1,) * (x.ndim - 1))     # noqa: E731
+    many = {k: rep(x) if k in ("u", "delta", "Bm", "Cm", "z", "h0") else x for k, x in v.items()}
+    L = _layer(B * copies, T, C, state=N, train=True, recompute=recompute)
+    lengths = [T, 77]
+    fwd, grad = _run_scan(L, many, rep(dy), rep(dhT), dtype, lengths * copies, True, False, recompute)
+    ref = seq.scan(**v, lengths=lengths, dy=dy, dhT=dhT)
+    size = seq.scan(**v, lengths=lengths, dy=dy, dhT=dhT, absolute=True)
+    got = dict(fwd, **grad)
+    for k in got:
+        if k in ("dA", "dD", "ddelta_bias"):
+            got[k] = got[k] / copies
+        else:
+            assert np.array_equal(got[k][:B], got[k][-B:]), k
+            got[k] = got[k][B:2 * B]
+    _check_scan(got, ref, size, B * copies, T, C, 1, N, dtype)
+
+
+def test_offsets_past_32_bits():
+    """Samples 2^30 elements apart: the third one's offsets pass 2^31 elements."""
+    torch = _torch()
+    B, T, C, N, far = 3, 40, 16, 4, 2 ** 30 + 8
+    v, dy, dhT = _scan_inputs(B, T, C, N, 1, "bfloat16", True, True, 21)
+    wide = torch.empty(2 * far + 8 * T * C, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(wide)
+    place = iter(range(8))
+
+    def at(x, buf=wide):
+        n = x.shape[-1]
+        t = buf[next(place) * T * C:].as_strided((B, T, n), (far, n, 1))
+        t.copy_(torch.from_numpy(np.ascontiguousarray(x.reshape(B, T, n))).bfloat16())
+        return t
+
+    u, delta, z, gdy, Bm, Cm = (at(x) for x in (v["u"], v["delta"], v["z"], dy, v["Bm"], v["Cm"]))
+    A, D, bias, h0 = (_dev(v[k]) for k in ("A", "D", "delta_bias", "h0"))
+    place = iter(range(8))
+    nan = np.full((B, T, C), np.nan)
+    y, du, dd, dz, cy, cdx = (at(nan, out) for _ in range(6))
+    dB, dC = at(nan[:, :, :N], out), at(nan[:, :, :N], out)
+    L = _layer(B, T, C, state=N, taps=4, train=True)
+    saved, hT = torch.empty(L.saved_shape, device="cuda"), torch.empty(B, C, N, device="cuda")
+    dA, dD, db, dh0 = (torch.empty_like(x) for x in (A, D, bias, h0))
+    opt = dict(D=D, z=z, delta_bias=bias)
+    L.scan_forward(u, delta, A, Bm, Cm, y, h0=h0, hT=hT, saved=saved, **opt)
+    L.scan_backward(u, delta, A, Bm, Cm, gdy, saved, du, dd, dA, dB, dC, dD=dD, dz=dz, ddelta_bias=db, dhT=_dev(dhT),
+                    dh0=dh0, **opt)
+    got = {k: x.double().cpu().numpy() for k, x in dict(y=y, hT=hT, du=du, ddelta=dd, dz=dz, dB=dB, dC=dC, dA=dA, dD=dD,
+                                                        ddelta_bias=db, dh0=dh0).items()}
+    ref, size = seq.scan(**v, dy=dy, dhT=dhT), seq.scan(**v, dy=dy, dhT=dhT, absolute=True)
+    _check_scan(got, ref, size, B, T, C, 1, N, "bfloat16")
+    w, dw = _dev(np.random.default_rng(1).normal(size=(C, 4))), torch.empty(C, 4, device="cuda")
+    L.conv_forward(u, w, None, cy)
+    L.conv_backward(u, w, None, gdy, cdx, dw)
+    hw = w.double().cpu().numpy()
+    ref, size = seq.conv(v["u"], hw, dy=dy), seq.conv(v["u"], hw, dy=dy, absolute=True)
+    _close("y", cy.double().cpu().numpy(), ref["y"], 1.1 * size["y"], "bfloat16", 20)
+    _close("dx", cdx.double().cpu().numpy(), ref["dx"], size["dx"], "bfloat16", 40)
 
 
 def test_scan_without_what_may_be_left_out():
@@ -433,6 +501,28 @@ def test_training_step_in_a_graph():
                 assert torch.equal(t[k], n[k]), (seed, k)
 
 
+def test_a_capture_on_another_stream_takes_the_handle_s_in():
+    torch = _torch()
+    B, T, C, N = 2, 64, 40, 16
+    mine, other = torch.cuda.Stream(), torch.cuda.Stream()
+    L, E = _layer(B, T, C, state=N, train=True, stream=mine), _layer(B, T, C, state=N, train=True)
+    t, outs = _train_tensors(B, T, C, N, 6)
+    t["saved"] = torch.empty(L.saved_shape, device="cuda")
+    _train_step(E, t)
+    want = {k: t[k].clone() for k in outs}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        _train_step(L, t)
+    for _ in range(3):
+        for k in outs:
+            t[k].fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in outs:
+            assert torch.equal(t[k], want[k]), k
+
+
 def test_calls_under_another_stream_are_ordered():
     torch = _torch()
     B, T, C, N = 2, 64, 128, 16
@@ -504,6 +594,9 @@ def test_refusals():
         lambda: L.bin_spikes(f(B, dtype=torch.int32), f(1, dtype=torch.int32), f(1, dtype=torch.int32), y),
         lambda: L.bin_spikes(f(B + 1, dtype=torch.int32), f(1, dtype=torch.int32), f(1, dtype=torch.int32), y, factor=0),
         lambda: L.bin_spikes(f(B + 1, dtype=torch.int32), f(1, dtype=torch.int32), f(1, dtype=torch.int32), y, factor=11),
+        lambda: L.conv_forward(x, w, None, x),                              # in place
+        lambda: L.scan_forward(x, x, A, bc, bc, x),
+        lambda: L.scan_step(x[:, 0], x[:, 0], A, bc[:, 0], bc[:, 0], st, st, x[:, 0]),
         lambda: L.pack(x, x),
         lambda: L.pack(x, snn.Packed.like(f(B, T, C + 1))),
         lambda: snn.Packed(f(B, T, C, dtype=torch.uint8), f(B, T, 2)),
@@ -514,6 +607,7 @@ def test_refusals():
         lambda: R.scan_backward(x, x, A, bc, bc, x, saved, z=x, **grads),   # a gate without its gradient
         lambda: R.scan_backward(x, x, A, bc, bc, x, saved, dz=y, **grads),
         lambda: R.scan_backward(x, x, A, bc, bc, q, saved, **grads),
+        lambda: R.scan_backward(x, x, A, bc, bc, x, saved, **dict(grads, ddelta=grads["du"])),      # two outputs in one
         lambda: R.scan_backward(x, x, A, bc, bc, x, saved, **dict(grads, dB=f(B, T, 2 * N).half())),
     ]
     for i, call in enumerate(bad):
