@@ -12,8 +12,8 @@
 // are taken in three steps of fixed order: within a wave by lane swaps, over
 // the workgroup's waves in LDS, over workgroups by scan_sums_kernel.
 //
-// Bound by the vector units: 75 instructions a wave and step of 16 channels,
-// 4 of them exponentials, and 21 for the elementwise work.  At 32 x 1000 x
+// Bound by the vector units: 80 instructions a wave and step of 16 channels,
+// 4 of them exponentials, and 16 for the elementwise work.  At 32 x 1000 x
 // 1024, 16 states, bf16, gated: 490 us, the vector units busy for 76% of it at
 // the two waves a SIMD that the registers allow, and 22 us for the sums over
 // workgroups; its 660 MB would take 130 us at a large copy's rate.

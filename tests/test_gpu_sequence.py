@@ -364,6 +364,32 @@ def test_scan_steps_and_parts_are_the_scan(dtype, N, G):
     _close("h", end.double().cpu().numpy(), ref["hT"], size["hT"], "float32", 32 * T + 64)
 
 
+@pytest.mark.parametrize("order", ["time first", "broadcast"])
+def test_strides_of_other_orders(order):
+    """[T][B][n] memory, and inputs that all samples share: the same results as from [B][T][n], bit for bit."""
+    torch = _torch()
+    B, T, C, N = 3, 45, 24, 8
+    t, outs = _train_tensors(B, T, C, N, 31)
+    if order == "broadcast":
+        for k in ("delta", "B", "C", "dy", "x"):
+            t[k] = t[k][:1].expand(B, -1, -1).contiguous()
+    L = _layer(B, T, C, state=N, train=True)
+    t["saved"] = torch.empty(L.saved_shape, device="cuda")
+    _train_step(L, t)
+    other = dict(t)
+    for k, v in t.items():
+        if k == "saved" or v.dim() != 3 or v.shape[:2] != (B, T):
+            other[k] = v if k not in outs else torch.empty_like(v)
+        elif order == "time first":
+            m = torch.empty(T, B, v.shape[2], dtype=v.dtype, device="cuda").transpose(0, 1)
+            other[k] = m.copy_(v) if k not in outs else m
+        else:
+            other[k] = v[:1].expand(B, -1, -1) if k in ("delta", "B", "C", "dy", "x") else v if k not in outs else torch.empty_like(v)
+    _train_step(L, other)
+    for k in outs:
+        assert torch.equal(t[k], other[k]), k
+
+
 def test_scan_gradients_are_the_same_from_call_to_call():
     torch = _torch()
     B, T, C, N = 3, 90, 100, 16
