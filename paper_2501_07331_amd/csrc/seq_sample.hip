@@ -9,17 +9,19 @@
 // What top-k, top-p and min-p keep is a beginning of the row in falling
 // order, which ends at a key (the score's bits, made to order as unsigned)
 // and a number of elements that have that key, the first ones by index.  The
-// end is found without a sort: a histogram of counts and weights over kBins
-// intervals of (m - z) / temperature, the interval in which the first of the
-// limits is passed, and again inside that interval over equal parts of its
-// keys, until a part is a single key.  The draw then goes over the row once
-// in index order.
+// end is found without a sort of the row: a histogram of counts and weights
+// over kBins intervals of (m - z) / temperature, the interval in which the
+// first of the limits is passed, and again inside that interval over equal
+// parts of its keys, until a part is a single key or has no more elements than
+// the workgroup threads: those are sorted.  The draw then goes over the row
+// once in index order.
 //
 // Three ways by size.  Rows of up to kWaveRow scores: a wave a row, an element
 // ranked by comparing it with every other.  Long rows that are too few to
 // fill the chip: a row is divided among workgroups for everything that reads
 // all of it, in five launches.  Otherwise a workgroup a row.
 #include <algorithm>
+#include <type_traits>
 
 #include "seq_device.h"
 #include "seq_sample.h"
@@ -28,7 +30,6 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr int kBins = 2048;
-constexpr int kList = 1024;                        // most elements of an interval that are ranked one by one
 
 // NaN orders below everything, as -inf.
 __device__ __forceinline__ unsigned key_of(float z) {
@@ -192,14 +193,15 @@ template <int NT>
 struct Work {
     u64 mass[kBins];
     unsigned count[kBins];
-    unsigned list[kList];
     u64 wmass[NT / 64];
     unsigned wcount[NT / 64];
     u64 above, inside_mass;        // weight above the cut interval, and of it
     unsigned n_above, inside;      // elements above it, and in it
     unsigned lo, hi, ends[3];      // its keys
     int bin, listed, token;
-    static_assert(kList <= kBins, "the list's weights take the histogram's place");
+    unsigned n_kept, last;         // how many of the list are kept, and the last one's index and key
+    unsigned last_key;
+    u64 kept_mass;
 };
 
 // Largest key of [begin, end) of a row, in every thread.
@@ -299,12 +301,16 @@ __device__ int find_cut(Work<NT>& w, u64 above, unsigned n_above, u64 limit, uns
     return cb;
 }
 
-// Where a row's kept elements end: those with a key above `key`, and the
-// first `count` of those that have it; `mass`: their weight.
+// Where a row's kept elements end: those with a key above `key`, and of those
+// that have it the first `count`, up to index `last`; `mass`: their weight.
+// count kOpen: not found yet, but among the few elements of an interval.
 struct End {
     unsigned key, count;
     u64 mass;
+    int last;
 };
+constexpr unsigned kOpen = ~0u;
+constexpr int kOpenMost = 1024;                    // most elements of an interval left open
 
 // The end in `inside` elements of one key: as many as the limits leave.
 __device__ __forceinline__ End end_in_key(const Row& r, unsigned key, unsigned inside, u64 inside_mass, u64 above,
@@ -313,11 +319,96 @@ __device__ __forceinline__ End end_in_key(const Row& r, unsigned key, unsigned i
     const u64 one = inside_mass / inside;
     if (above >= limit) count = 0;
     else if (one) count = (unsigned)min((u64)count, (limit - above - 1) / one + 1);
-    return End{key, count, above + one * count};
+    return End{key, count, above + one * count, 0x7fffffff};
+}
+
+// An element of the list: by falling key, then by rising index.
+__device__ __forceinline__ u64 in_list(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
+__device__ __forceinline__ unsigned list_key(u64 x) { return (unsigned)(x >> 32); }
+__device__ __forceinline__ int list_index(u64 x) { return (int)~(unsigned)x; }
+
+// x of lane ^ J.
+template <int J>
+__device__ __forceinline__ unsigned lane_xor(unsigned x) {
+    constexpr int kQuadMirror = 0x1B;
+    auto dpp = [](unsigned v, auto ctrl) {
+        return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, true);
+    };
+    if constexpr (J == 1) return dpp(x, std::integral_constant<int, kQuadXor1>());
+    if constexpr (J == 2) return dpp(x, std::integral_constant<int, kQuadXor2>());
+    if constexpr (J == 4) {                            // 7 - i, then 3 - i within each quad
+        return dpp(dpp(x, std::integral_constant<int, kHalfMirror>()), std::integral_constant<int, kQuadMirror>());
+    }
+    if constexpr (J == 8) return dpp(x, std::integral_constant<int, kRor + 8>());
+    if constexpr (J == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+}
+
+// Exchanges over J, J / 2, ... 1 lanes of a bitonic network; down: the larger
+// element goes to the lower lane.
+template <int J>
+__device__ __forceinline__ u64 lane_merge(u64 x, bool down) {
+    const u64 y = (u64)lane_xor<J>((unsigned)(x >> 32)) << 32 | lane_xor<J>((unsigned)x);
+    x = (x < y) == (down == !(threadIdx.x & J)) ? y : x;
+    if constexpr (J > 1) return lane_merge<J / 2>(x, down);
+    return x;
+}
+
+// The end among the n <= NT elements of the list, which lies in w.mass and is
+// sorted there, one element a thread, by a bitonic network: exchanges within a
+// wave are between its lanes' registers.  w.n_kept of the elements are kept.
+template <int NT>
+__device__ End end_in_list(const Row& r, unsigned n, u64 above, unsigned n_above, u64 limit, unsigned hi, Work<NT>& w) {
+    static_assert(NT <= kBins, "the list takes the histogram's place");
+    const unsigned tid = threadIdx.x, wave = tid / 64;
+    if (tid == 0) w.n_kept = 0, w.last_key = hi, w.last = (unsigned)-1, w.kept_mass = above;
+    __syncthreads();
+    u64 x = tid < n ? w.mass[tid] : 0;                 // 0 is below every element
+    if (wave * 64 < n) {
+        x = lane_merge<1>(x, !(tid & 2));
+        x = lane_merge<2>(x, !(tid & 4));
+        x = lane_merge<4>(x, !(tid & 8));
+        x = lane_merge<8>(x, !(tid & 16));
+        x = lane_merge<16>(x, !(tid & 32));
+        x = lane_merge<32>(x, !(tid & 64));
+    }
+    for (unsigned k = 128; k < 2 * n; k *= 2) {        // up to the power of two that holds n
+        for (unsigned j = k / 2; j >= 64; j /= 2) {
+            __syncthreads();
+            w.mass[tid] = x;
+            __syncthreads();
+            const u64 y = w.mass[tid ^ j];
+            x = (x < y) == (!(tid & k) == !(tid & j)) ? y : x;
+        }
+        x = lane_merge<32>(x, !(tid & k));
+    }
+    __syncthreads();
+    w.mass[tid] = x;
+    bool kept;
+    const u64 v = tid < n ? r.weight(score_of(list_key(x)), kept) : 0;
+    const u64 sum = wave_scan(v);
+    if (tid % 64 == 63) w.wmass[wave] = sum;
+    __syncthreads();
+    u64 before = above + sum - v;
+    for (unsigned k = 0; k < wave; ++k) before += w.wmass[k];
+    const unsigned rank = n_above + tid;
+    // one element is the last that the limits leave
+    if (tid < n && rank < (unsigned)r.top_k && before < limit &&
+        (rank + 1 >= (unsigned)r.top_k || before + v >= limit || tid + 1 == n)) {
+        w.n_kept = tid + 1, w.last_key = list_key(x), w.last = list_index(x), w.kept_mass = before + v;
+    }
+    __syncthreads();
+    return End{w.last_key, kOpen, w.kept_mass, (int)w.last};
 }
 
 // From the histogram over the intervals of depth, for [0, n) of the row.
-template <class T, int NT>
+// DEFER: an interval of few elements is left to the caller, as w.above,
+// w.n_above, w.inside, w.lo and w.hi.
+template <class T, int NT, bool DEFER>
 __device__ End find_end(const SampleArgs& a, int row, const Row& r, unsigned top, u64 limit, Work<NT>& w) {
     const int tid = threadIdx.x;
     u64 above = 0;
@@ -326,7 +417,7 @@ __device__ End find_end(const SampleArgs& a, int row, const Row& r, unsigned top
     for (int level = 0;; ++level) {
         const int cb = find_cut(w, above, n_above, limit, (unsigned)r.top_k);
         above = w.above, n_above = w.n_above;
-        if (cb == kBins) return End{0, 0, above};  // nothing is cut off
+        if (cb == kBins) return End{0, 0, above, 0};  // nothing is cut off
         const unsigned inside = w.inside;
         const u64 inside_mass = w.inside_mass;
         if (tid == 0) w.listed = 0;
@@ -364,46 +455,17 @@ __device__ End find_end(const SampleArgs& a, int row, const Row& r, unsigned top
         lo = level ? w.lo : max(w.ends[0], w.ends[2]), hi = level ? w.hi : w.ends[1];
         if (lo == hi) return end_in_key(r, lo, inside, inside_mass, above, n_above, limit);
         const float zlo = score_of(lo), zhi = score_of(hi);
-        if (inside <= kList) {
-            // few elements: each is placed by comparison with all of them
-            each_score<T, NT, 4>(a, row, 0, a.n, [&](int, float z) {
+        if (DEFER && inside <= kOpenMost) {
+            if (tid == 0) w.lo = lo, w.hi = hi;
+            return End{hi, kOpen, 0, 0};
+        }
+        if (inside <= NT) {
+            each_score<T, NT, 4>(a, row, 0, a.n, [&](int i, float z) {
                 if (!(z >= zlo && z <= zhi)) return;
                 const int at = atomicAdd(&w.listed, 1);
-                if (at < kList) w.list[at] = key_of(z);     // always: they are the interval's `inside`
+                if (at < NT) w.mass[at] = in_list(key_of(z), i);     // always: they are the interval's `inside`
             });
-            __syncthreads();
-            for (unsigned e = tid; e < inside; e += NT) {
-                bool kept;
-                w.mass[e] = r.weight(score_of(w.list[e]), kept);
-            }
-            __syncthreads();
-            // G neighbouring lanes an element, each over its share of the list
-            const unsigned G = inside <= NT / 16 ? 16 : inside <= NT / 4 ? 4 : 1;
-            for (unsigned e = tid / G; e < inside; e += NT / G) {
-                const unsigned key = w.list[e];
-                u64 bm = 0, em = 0;
-                unsigned bc = 0, ec = 0;
-#pragma unroll 4
-                for (unsigned i = tid % G; i < inside; i += G) {
-                    const unsigned other = w.list[i];
-                    const u64 v = w.mass[i];
-                    bm += other > key ? v : 0, bc += other > key;
-                    em += other == key ? v : 0, ec += other == key;
-                }
-                for (unsigned d = 1; d < G; d *= 2) {
-                    bm += __shfl_xor(bm, d), em += __shfl_xor(em, d);
-                    bc += __shfl_xor(bc, d), ec += __shfl_xor(ec, d);
-                }
-                bm += above, bc += n_above;
-                const unsigned k = (unsigned)r.top_k;
-                // the limits are passed among this key's elements; they all find the same
-                if (bc <= k && bm < limit && (bc + ec > k || bm + em >= limit)) {
-                    w.lo = key, w.above = bm, w.n_above = bc;
-                    w.inside = ec, w.inside_mass = em;
-                }
-            }
-            __syncthreads();
-            return end_in_key(r, w.lo, w.inside, w.inside_mass, w.above, w.n_above, limit);
+            return end_in_list(r, inside, above, n_above, limit, hi, w);
         }
         sh = 0;
         while ((hi - lo) >> sh >= (unsigned)kBins) ++sh;
@@ -465,7 +527,7 @@ __device__ void draw(const SampleArgs& a, int row, int begin, int end, const Row
         for (int j = 0; j < VW; ++j) {
             const unsigned key = i + j < end ? key_of(z[j]) : 0;
             if (e.key && key == e.key && v[j]) {
-                if (before >= e.count) v[j] = 0;
+                if (before >= e.count || i + j > e.last) v[j] = 0;
                 ++before;
                 tm += v[j];
             }
@@ -512,7 +574,7 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a) {
         return;
     }
     const u64 all = depth_histogram<T, NT>(a, row, 0, a.n, r, w);
-    const End e = find_end<T, NT>(a, row, r, top, r.mass_limit(all), w);
+    const End e = find_end<T, NT, false>(a, row, r, top, r.mass_limit(all), w);
     draw<T, NT>(a, row, 0, a.n, r, e, share(e.mass, r.u, false), 0, 0, w);
 }
 
@@ -599,13 +661,18 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
 
 // ------------------------------------------------------------------ rows divided among workgroups
 
+// Workgroups of 2048 scores and more, where the rows alone give fewer
+// workgroups than half the chip's CUs.
+constexpr int kPartRows = 128, kPartAll = 1024, kPartScores = 2048, kPartMin = 16384;
 constexpr int kPartNT = 256;
 
 // What the launches of a divided row hand on: [rows] of
 struct RowState {
-    u64 all, goal, end_mass;
+    u64 goal, end_mass;
+    u64 above, limit;              // open: the interval that the kept elements end in
+    unsigned n_above, lo, hi, listed;
     unsigned top, end_key, end_count;
-    int done;                      // answered already
+    int done, open;                // answered already; the end is still to be found
 };
 struct PartState {                 // [rows][parts]
     u64 all, mass;                 // weight, and that of the kept elements above the last key
@@ -621,6 +688,10 @@ __device__ __forceinline__ u64* hist_mass(const SampleArgs& a) {
 }
 __device__ __forceinline__ unsigned* hist_count(const SampleArgs& a) {
     return reinterpret_cast<unsigned*>(hist_mass(a) + (long long)a.rows * kBins);
+}
+// An open interval's elements, in any order.
+__device__ __forceinline__ u64* open_list(const SampleArgs& a, int row) {
+    return reinterpret_cast<u64*>(hist_count(a) + (long long)a.rows * kBins) + (long long)row * kOpenMost;
 }
 
 // Largest keys; the row's histogram is cleared.
@@ -689,31 +760,44 @@ __global__ void __launch_bounds__(1024) sample_end_kernel(SampleArgs a) {
         w.count[i] = hist_count(a)[(long long)row * kBins + i];
     }
     __syncthreads();
-    const End e = find_end<T, 1024>(a, row, r, top, r.mass_limit(all), w);
+    const u64 limit = r.mass_limit(all);
+    const End e = find_end<T, 1024, true>(a, row, r, top, limit, w);
     if (tid == 0) {
+        s.open = e.count == kOpen;
+        s.above = w.above, s.n_above = w.n_above, s.limit = limit;
+        s.lo = w.lo, s.hi = w.hi, s.listed = 0;
         s.end_key = e.key, s.end_count = e.count, s.end_mass = e.mass;
         s.goal = share(e.mass, r.u, false);
     }
 }
 
-// The parts' kept weight.
+// The parts' kept weight, without the last key's elements, which are counted,
+// or without an open interval's, which are listed.
 template <class T>
 __global__ void __launch_bounds__(kPartNT) sample_parts_kernel(SampleArgs a) {
     __shared__ u64 mass[kPartNT / 64];
     __shared__ unsigned ties[kPartNT / 64];
     const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
     const int begin = part * a.part_len, end = min(a.n, begin + a.part_len);
-    const RowState s = row_state(a)[row];
+    RowState* state = row_state(a) + row;
+    const RowState s = *state;
     if (s.done) return;
     Row r(a, row);
     r.m = score_of(s.top);
     u64 m = 0;
     unsigned t = 0;
-    const float last = s.end_key ? score_of(s.end_key) : -INFINITY;
-    each_score<T, kPartNT, 2>(a, row, begin, end, [&](int, float z) {
-        if (!(z >= last && z > -INFINITY)) return;
-        if (z == last) {
-            ++t;                                   // min-p keeps the last key: the end is among what it keeps
+    const float last = s.end_key ? score_of(s.end_key) : -INFINITY, low = s.open ? score_of(s.lo) : last;
+    u64* list = open_list(a, row);
+    each_score<T, kPartNT, 2>(a, row, begin, end, [&](int i, float z) {
+        if (!(z >= low && z > -INFINITY)) return;
+        if (z <= last) {
+            // min-p keeps these: the end is among what it keeps
+            if (s.open) {
+                const unsigned at = atomicAdd(&state->listed, 1u);
+                if (at < (unsigned)kOpenMost) list[at] = in_list(key_of(z), i);   // always: they are at most that many
+            } else {
+                ++t;
+            }
             return;
         }
         bool kept;
@@ -729,19 +813,35 @@ __global__ void __launch_bounds__(kPartNT) sample_parts_kernel(SampleArgs a) {
     p.mass = m, p.ties = t;
 }
 
-// The part in which the running sum passes the goal, and the index in it.
+// The end in an open interval, if there is one; the part in which the running
+// sum passes the goal, and the index in it.
+constexpr int kDrawNT = kOpenMost;
 template <class T>
-__global__ void __launch_bounds__(kPartNT) sample_draw_kernel(SampleArgs a) {
-    __shared__ Work<kPartNT> w;
-    const int row = blockIdx.x;
+__global__ void __launch_bounds__(kDrawNT) sample_draw_kernel(SampleArgs a) {
+    __shared__ Work<kDrawNT> w;
+    __shared__ u64 more[kPartAll];                 // an open interval's kept weight, by part
+    const int row = blockIdx.x, tid = threadIdx.x;
     const RowState s = row_state(a)[row];
     if (s.done) return;
     Row r(a, row);
     r.m = score_of(s.top);
-    const End e{s.end_key, s.end_count, s.end_mass};
-    u64 run = 0, one = 0;
+    End e{s.end_key, s.end_count, s.end_mass, 0x7fffffff};
+    u64 goal = s.goal;
+    if (s.open) {
+        const unsigned listed = min(s.listed, (unsigned)kOpenMost);
+        for (int i = tid; i < a.parts; i += kDrawNT) more[i] = 0;
+        for (unsigned i = tid; i < listed; i += kDrawNT) w.mass[i] = open_list(a, row)[i];
+        e = end_in_list(r, listed, s.above, s.n_above, s.limit, s.hi, w);
+        goal = share(e.mass, r.u, false);
+        for (unsigned i = tid; i < w.n_kept; i += kDrawNT) {
+            bool kept;
+            atomicAdd(&more[list_index(w.mass[i]) / a.part_len], r.weight(score_of(list_key(w.mass[i])), kept));
+        }
+        __syncthreads();
+    }
+    u64 one = 0;
     unsigned ties = 0;
-    if (e.key) {
+    if (!s.open && e.key) {
         bool kept;
         one = r.weight(score_of(e.key), kept);
     }
@@ -749,11 +849,12 @@ __global__ void __launch_bounds__(kPartNT) sample_draw_kernel(SampleArgs a) {
     int part = a.parts - 1;
     u64 mass = 0;
     for (int base = 0; base < a.parts; base += 64) {
-        const int k = base + threadIdx.x % 64;
-        const PartState p = k < a.parts ? part_state(a)[row * a.parts + k] : PartState{};
+        const int k = base + tid % 64;
+        PartState p = k < a.parts ? part_state(a)[row * a.parts + k] : PartState{};
+        if (s.open) p.mass += k < a.parts ? more[k] : 0, p.ties = 0;
         const u64 m1 = mass + wave_scan(p.mass);
         const unsigned t1 = ties + wave_scan(p.ties);
-        const u64 to = __ballot(k < a.parts && m1 + one * min(t1, e.count) > s.goal);
+        const u64 to = __ballot(k < a.parts && m1 + one * min(t1, e.count) > goal);
         const int f = to ? __ffsll(to) - 1 : 63;
         const u64 m0 = __shfl(m1 - p.mass, f);
         const unsigned t0 = __shfl(t1 - p.ties, f);
@@ -764,9 +865,8 @@ __global__ void __launch_bounds__(kPartNT) sample_draw_kernel(SampleArgs a) {
         }
         mass = __shfl(m1, 63), ties = __shfl(t1, 63);
     }
-    run = mass + one * min(ties, e.count);
     const int begin = part * a.part_len;
-    draw<T, kPartNT>(a, row, begin, min(a.n, begin + a.part_len), r, e, s.goal, run, ties, w);
+    draw<T, kDrawNT>(a, row, begin, min(a.n, begin + a.part_len), r, e, goal, mass + one * min(ties, e.count), ties, w);
 }
 
 template <class T>
@@ -784,7 +884,7 @@ hipError_t sample(const SampleArgs& a, hipStream_t s) {
         sample_hist_kernel<T><<<grid, kPartNT, 0, s>>>(a);
         sample_end_kernel<T><<<a.rows, 1024, 0, s>>>(a);
         sample_parts_kernel<T><<<grid, kPartNT, 0, s>>>(a);
-        sample_draw_kernel<T><<<a.rows, kPartNT, 0, s>>>(a);
+        sample_draw_kernel<T><<<a.rows, kDrawNT, 0, s>>>(a);
     } else if (a.n <= 4096)
         sample_row_kernel<T, 256><<<a.rows, 256, 0, s>>>(a);
     else
@@ -794,9 +894,6 @@ hipError_t sample(const SampleArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups of 2048 scores and more, where the rows alone give fewer
-// workgroups than half the chip's CUs.
-constexpr int kPartRows = 128, kPartAll = 1024, kPartScores = 2048, kPartMin = 16384;
 int sample_parts(int rows, int n) {
     if (n < kPartMin || rows > kPartRows) return 1;
     return std::min(n / kPartScores, kPartAll / rows);
@@ -804,7 +901,7 @@ int sample_parts(int rows, int n) {
 size_t sample_scratch(int rows, int n) {
     if (n < kPartMin) return 0;
     const size_t r = std::min(rows, kPartRows);    // and rows x parts is at most kPartAll
-    return r * (sizeof(RowState) + kBins * 12) + kPartAll * sizeof(PartState);
+    return r * (sizeof(RowState) + kBins * 12 + kOpenMost * sizeof(u64)) + kPartAll * sizeof(PartState);
 }
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t s) {

@@ -116,6 +116,21 @@ def test_a_long_row_and_the_ends_of_u():
     _run(z, u, "bfloat16", top_p=np.full(6, 0.95), top_k=[0, 0, 1000, 60000, 12345, 0])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_few_equal_scores_far_apart(dtype):
+    """The limits fall among a few elements that three close values share, all over a long row: each place of the border,
+    and draws from the first element to the last one kept."""
+    r = np.random.default_rng(21)
+    R, V, few = 48, 33001, 40
+    z = (r.normal(size=(R, V)) * 0.5 - 12).astype(np.float32)
+    for k in range(R):
+        z[k, r.choice(V, few, replace=False)] = r.choice([2.0, 2.015625, 2.03125], few)
+    u = np.where(np.arange(R) % 3 == 0, 1 - 2.0 ** -24, np.where(np.arange(R) % 3 == 1, 0.0, r.random(R)))
+    _run(z, u, dtype, True, top_k=np.arange(1, R + 1))
+    _run(z, u, dtype, top_p=np.linspace(0.0, 1.0, R))
+    _run(z, u, dtype, top_k=np.full(R, few + 5), top_p=r.uniform(0.3, 1, R), min_p=np.where(np.arange(R) % 2, 0.98, 0.0))
+
+
 def test_a_handle_serves_smaller_calls():
     """Rows and scores below the handle's: a row is divided otherwise for each call."""
     import torch
