@@ -98,8 +98,8 @@ void snn_seq_destroy(snn_seq* seq);                   /* waits for its stream */
  * SNN_E4M3 (counts past 2048 round in SNN_F16, past 256 in SNN_BF16).
  * bin_spikes reads snn.h's input lists, bin_records one layer's records of
  * [batch][capacity] (stored records only: min(count, capacity)).  A sample's
- * events are in order of their step; an event outside [0, T) x [0, n) is left
- * out.
+ * events are in order of their step, a neuron has at most one a step (as in
+ * snn.h); an event outside [0, T) x [0, n) is left out.
  */
 int snn_seq_bin_spikes(snn_seq* seq, const snn_spikes_in* in, int32_t n, int32_t factor,
                        const snn_tensor* dst);
@@ -189,7 +189,9 @@ int snn_seq_saved(const snn_seq* seq, int64_t* floats);   /* floats of `saved` (
  * the packed values.  saved: as the forward wrote it, or NULL: the states are
  * computed again from u, delta, B and h0 (SNN_SEQ_RECOMPUTE), which is what
  * belongs to packed u and delta: the states saved from the unpacked ones are
- * not those of the packed values.  h0 is read only then.  dD, ddelta_bias and
+ * not those of the packed values.  h0 is read only then, and where states grow
+ * (A delta' > 0) exp of the sum of A delta' over the steps has to stay in
+ * fp32's range then (infinity times zero is NaN).  dD, ddelta_bias and
  * dh0 may be NULL (not wanted); dz.data is NULL exactly where z.data is. */
 typedef struct {
     snn_tensor u, delta, B, C, z, dy, du, ddelta, dB, dC, dz;

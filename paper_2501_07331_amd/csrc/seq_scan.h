@@ -66,15 +66,15 @@ __device__ __forceinline__ void through_parts(const ScanArgs& a, const float* ca
         for (int i = 0; i < 4; ++i) {
             const long long p = at + (long long)(first + dir * (j + i < n ? j + i : j)) * a.channels;
             end[i] = *reinterpret_cast<const float4*>(carry + p * np + 4 * q);
-            sum[i] = a.dsum[p];
+            sum[i] = 0.5f * a.dsum[p];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (j + i >= n) break;
-            h[0] = fmaf(exp2_fast(sum[i] * A2[0]), h[0], end[i].x);
-            h[1] = fmaf(exp2_fast(sum[i] * A2[1]), h[1], end[i].y);
-            h[2] = fmaf(exp2_fast(sum[i] * A2[2]), h[2], end[i].z);
-            h[3] = fmaf(exp2_fast(sum[i] * A2[3]), h[3], end[i].w);
+            h[0] = exp2_twice(sum[i] * A2[0], h[0], end[i].x);
+            h[1] = exp2_twice(sum[i] * A2[1], h[1], end[i].y);
+            h[2] = exp2_twice(sum[i] * A2[2], h[2], end[i].z);
+            h[3] = exp2_twice(sum[i] * A2[3], h[3], end[i].w);
         }
     }
 }

@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, float* carry
         for (int j = 0; j < 8; ++j) {
             if (k + j >= a.chunks) break;
             carry[(at + j * step) * NP + n] = h;
-            h = fmaf(exp2_fast(sum[j] * A2), h, end[j]);
+            h = exp2_twice(0.5f * sum[j] * A2, h, end[j]);
         }
         at += 8 * step;
     }

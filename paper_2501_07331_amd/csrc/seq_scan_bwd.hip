@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(256) scan_join_back_kernel(ScanArgs a, int NP)
         for (int j = 0; j < 8; ++j) {
             if (k - j < 0) break;
             a.carry[(at - j * step) * NP + n] = g;
-            g = fmaf(exp2_fast(sum[j] * A2), g, start[j]);
+            g = exp2_twice(0.5f * sum[j] * A2, g, start[j]);
         }
     }
 }

@@ -364,6 +364,41 @@ def test_scan_steps_and_parts_are_the_scan(dtype, N, G):
     _close("h", end.double().cpu().numpy(), ref["hT"], size["hT"], "float32", 32 * T + 64)
 
 
+@pytest.mark.parametrize("T", [700, 4000])
+def test_states_that_grow_from_zero(T):
+    """exp(A sum delta') over a part of the time axis overflows, and what it multiplies is zero: the states before the
+    inputs begin, the adjoints behind the last gradient.  Four steps of decays with 4.7 roundings of their argument and
+    four more each, sums over 5 states and 40 channels: 128 roundings hold them."""
+    torch = _torch()
+    B, C, N = 1, 40, 5
+    r = np.random.default_rng(T)
+    f = lambda *s: torch.from_numpy(r.normal(size=s)).float()           # noqa: E731
+    L = _layer(B, T, C, state=N, train=True)
+    A = torch.from_numpy(r.uniform(2.8, 3.2, size=(C, N))).float()
+    A[::2] *= -1
+    u, dy, zero = torch.zeros(B, T, C), torch.zeros(B, T, C), torch.zeros(B, T, C)
+    u[:, -4:], dy[:, :3], delta = f(B, 4, C), f(B, 3, C), torch.ones(B, T, C)
+    Bm, Cm = f(B, T, N), f(B, T, N)
+    g = {k: x.cuda() for k, x in dict(u=u, dy=dy, zero=zero, delta=delta, A=A, B=Bm, C=Cm).items()}
+    y, hT, saved = torch.empty(B, T, C, device="cuda"), torch.empty(B, C, N, device="cuda"), torch.empty(L.saved_shape, device="cuda")
+    o = dict(du=torch.empty_like(y), ddelta=torch.empty_like(y), dA=torch.empty(C, N, device="cuda"),
+             dB=torch.empty(B, T, N, device="cuda"), dC=torch.empty(B, T, N, device="cuda"))
+
+    def oracle(u, dy=None):
+        v = [x.double().numpy() for x in (u, delta, A, Bm.view(B, T, 1, N), Cm.view(B, T, 1, N))]
+        return [seq.scan(*v, plus=False, dy=None if dy is None else dy.double().numpy(), absolute=x) for x in (False, True)]
+
+    L.scan_forward(g["u"], g["delta"], g["A"], g["B"], g["C"], y, hT=hT, softplus=False)
+    ref, size = oracle(u)
+    for k, x in dict(y=y, hT=hT).items():
+        _close(k, x.double().cpu().numpy(), ref[k], size[k], "float32", 128)
+    L.scan_forward(g["zero"], g["delta"], g["A"], g["B"], g["C"], y, saved=saved, softplus=False)
+    L.scan_backward(g["zero"], g["delta"], g["A"], g["B"], g["C"], g["dy"], saved, softplus=False, **o)
+    ref, size = oracle(zero, dy)
+    for k, x in o.items():
+        _close(k, x.double().cpu().numpy(), ref[k].reshape(x.shape), size[k].reshape(x.shape), "float32", 128)
+
+
 @pytest.mark.parametrize("order", ["time first", "broadcast"])
 def test_strides_of_other_orders(order):
     """[T][B][n] memory, and inputs that all samples share: the same results as from [B][T][n], bit for bit."""
