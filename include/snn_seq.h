@@ -35,7 +35,8 @@
  * and changes neither states nor gradients.  A sample of length 0 ends in the
  * state it started from.
  *
- * Errors: SNN_EINVAL (bad sizes, types, strides or NULL pointers; nothing is
+ * Errors: SNN_EINVAL (bad sizes, types, strides, NULL pointers, outputs that
+ * are inputs, sizes whose launches would have 2^32 threads and more; nothing is
  * enqueued), SNN_ENOMEM, SNN_EDEVICE; snn_seq_last_error has the message.
  */
 #ifndef SNN_SEQ_H
@@ -245,6 +246,7 @@ typedef struct {
     float* logprob;          /* [rows] or NULL */
 } snn_sample_args;
 #define SNN_SAMPLE_MAX_N (1 << 24)
+/* rows < 2^22 - 63, n <= SNN_SAMPLE_MAX_N */
 int snn_sampler_create(int32_t rows, int32_t n, void* hip_stream, snn_sampler** out);
 int snn_sampler_sample(snn_sampler* s, const snn_sample_args* a);
 const char* snn_sampler_last_error(const snn_sampler* s);

@@ -50,6 +50,9 @@ void time_parts(int T, long long waves, int enough, int fill, int* parts, int* l
     *parts = (T + *len - 1) / *len;
 }
 
+// A launch has at most 2^32 - 1 threads along a dimension; some blocks' roundings are left free.
+bool launchable(long long threads) { return threads <= 0xffff0000ll; }
+
 }  // namespace
 
 struct snn_seq {
@@ -204,7 +207,12 @@ extern "C" int snn_seq_create(const snn_seq_opts* o, snn_seq** out) {
     const int np = scan_np(o->state), cb = scan_cb(np);
     const int gblocks = (o->channels / o->groups + cb - 1) / cb;
     const long long wgs = (long long)o->batch * o->groups * gblocks;
-    if (wgs > 0x7fffffffll / 2) return create_fail(SNN_EINVAL, "batch x channel blocks exceed a launch", nullptr);
+    if (!launchable(wgs * cb * (np / 4))) return create_fail(SNN_EINVAL, "batch x channels exceed a launch", nullptr);
+    if (!launchable((long long)o->batch * (o->taps - 1) * o->channels))
+        return create_fail(SNN_EINVAL, "batch x taps x channels exceed a launch", nullptr);
+    // the sums of the scan's gradients: an element of dB and dC a thread, 8 for a column of the others
+    if ((o->flags & SNN_SEQ_TRAIN) && !launchable(2ll * o->batch * o->T * o->groups * o->state + 8ll * o->channels * (np + 2)))
+        return create_fail(SNN_EINVAL, "batch x T x groups x state exceed a launch", nullptr);
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return create_fail(SNN_EDEVICE, "hipGetDevice", hipGetErrorString(e));
@@ -280,6 +288,7 @@ static int bin(snn_seq* s, BinArgs& a, int n, int factor, const snn_tensor* dst)
     a.factor = factor;
     a.rows = (s->o.T + factor - 1) / factor;
     ARG(out_arg(s, *dst, "dst", n, a.rows, -1, &a.y));
+    ARG(distinct(s, {a.offsets, a.count, a.step, a.neuron}, {dst->data}));
     a.past = (size_t)a.batch * a.rows * n * (dst->dtype == SNN_F32 ? 4 : 2) > (32u << 20);
     // rows a workgroup: 16 KiB of counts, so that several workgroups share a CU, or one row
     a.tile = std::min(a.rows, std::max(1, 8192 / n));
@@ -328,7 +337,7 @@ static int pack_args(snn_seq* s, int n, const snn_tensor* x, const snn_tensor* q
     a->batch = s->o.batch;
     a->T = s->o.T;
     a->n = n;
-    if ((long long)a->batch * a->T * ((n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK) > (1ll << 34))
+    if (!launchable((long long)a->batch * a->T * ((n + SNN_SEQ_BLOCK - 1) / SNN_SEQ_BLOCK) * (SNN_SEQ_BLOCK / 8)))
         return fail(s, SNN_EINVAL, "batch x T x n exceeds a launch");
     return SNN_OK;
 }
@@ -337,6 +346,7 @@ extern "C" int snn_seq_pack(snn_seq* s, int32_t n, const snn_tensor* x, const sn
     SEQ_ENTER(s);
     PackArgs a{};
     ARG(pack_args(s, n, x, q, true, &a));
+    ARG(distinct(s, {x->data}, {q->data, q->scale}));
     SEQ_TRY(s, launch_pack(a, x->dtype, s->stream));
     return SNN_OK;
 }
@@ -345,6 +355,7 @@ extern "C" int snn_seq_unpack(snn_seq* s, int32_t n, const snn_tensor* q, const 
     SEQ_ENTER(s);
     PackArgs a{};
     ARG(pack_args(s, n, x, q, false, &a));
+    ARG(distinct(s, {q->data, q->scale}, {x->data}));
     SEQ_TRY(s, launch_unpack(a, x->dtype, s->stream));
     return SNN_OK;
 }
@@ -376,7 +387,7 @@ extern "C" int snn_seq_conv_forward(snn_seq* s, const snn_seq_conv* c) {
     SEQ_ENTER(s);
     ConvArgs a{};
     ARG(conv_args(s, c, s->o.T, &a));
-    ARG(distinct(s, {c->x.data, c->w, c->bias, c->state}, {c->y.data, c->state_out}));
+    ARG(distinct(s, {c->x.data, c->w, c->bias, c->state, c->lengths}, {c->y.data, c->state_out}));
     SEQ_TRY(s, launch_conv_forward(a, c->x.dtype, s->stream));
     return SNN_OK;
 }
@@ -421,7 +432,7 @@ extern "C" int snn_seq_conv_backward(snn_seq* s, const snn_seq_conv_grad* c) {
     a.silu = c->silu != 0;
     a.tiles = conv_tiles(T, C, s->o.taps);
     a.part = s->cpart;
-    ARG(distinct(s, {c->x.data, c->x.scale, c->dy.data, c->w, c->bias, c->state, c->dstate_out},
+    ARG(distinct(s, {c->x.data, c->x.scale, c->dy.data, c->w, c->bias, c->state, c->dstate_out, c->lengths},
                  {c->dx.data, c->dw, c->dbias, c->dstate}));
     SEQ_TRY(s, launch_conv_backward(a, type, s->stream));
     return SNN_OK;
@@ -461,7 +472,8 @@ extern "C" int snn_seq_scan_forward(snn_seq* s, const snn_seq_scan* c) {
     SEQ_ENTER(s);
     ScanArgs a{};
     ARG(scan_args(s, c, s->o.T, &a));
-    ARG(distinct(s, {c->u.data, c->delta.data, c->B.data, c->C.data, c->z.data, c->A, c->D, c->delta_bias, c->h0},
+    ARG(distinct(s, {c->u.data, c->delta.data, c->B.data, c->C.data, c->z.data, c->A, c->D, c->delta_bias, c->h0,
+                     c->lengths},
                  {c->y.data, c->hT, c->saved}));
     SEQ_TRY(s, launch_scan_forward(a, c->u.dtype, s->stream));
     return SNN_OK;
@@ -536,7 +548,7 @@ extern "C" int snn_seq_scan_backward(snn_seq* s, const snn_seq_scan_grad* c) {
     a.lengths = c->lengths;
     a.softplus = c->softplus != 0;
     ARG(distinct(s, {c->u.data, c->u.scale, c->delta.data, c->delta.scale, c->B.data, c->C.data, c->z.data, c->z.scale,
-                     c->dy.data, c->A, c->D, c->delta_bias, c->h0, c->dhT, c->saved},
+                     c->dy.data, c->A, c->D, c->delta_bias, c->h0, c->dhT, c->saved, c->lengths},
                  {c->du.data, c->ddelta.data, c->dB.data, c->dC.data, c->dz.data, c->dA, c->dD, c->ddelta_bias, c->dh0}));
     scan_sizes(s, true, &a);
     if (!c->saved) {
@@ -568,7 +580,7 @@ extern "C" int snn_sampler_create(int32_t rows, int32_t n, void* hip_stream, snn
     g_seq_err[0] = 0;
     if (!out) return create_fail(SNN_EINVAL, "NULL out", nullptr);
     *out = nullptr;
-    if (rows < 1) return create_fail(SNN_EINVAL, "rows must be at least 1", nullptr);
+    if (rows < 1 || !launchable(rows * 1024ll)) return create_fail(SNN_EINVAL, "rows must be 1 .. 2^22 - 64", nullptr);
     if (n < 1 || n > SNN_SAMPLE_MAX_N) return create_fail(SNN_EINVAL, "n must be 1 .. SNN_SAMPLE_MAX_N", nullptr);
     int dev = 0;
     const hipError_t e = hipGetDevice(&dev);
@@ -619,6 +631,11 @@ extern "C" int snn_sampler_sample(snn_sampler* s, const snn_sample_args* c) {
     const void* words[] = {c->u, c->temperature, c->top_k, c->top_p, c->min_p, c->token, c->logprob};
     for (const void* p : words)
         if (reinterpret_cast<uintptr_t>(p) % 4) return fail(s, SNN_EINVAL, "a misaligned array of rows", nullptr);
+    const void* in[] = {c->scores, c->u, c->temperature, c->top_k, c->top_p, c->min_p};
+    for (const void* p : in)
+        if (p && (p == c->token || p == c->logprob)) return fail(s, SNN_EINVAL, "an output is an input", nullptr);
+    if (c->logprob && static_cast<const void*>(c->token) == c->logprob)
+        return fail(s, SNN_EINVAL, "two outputs are one", nullptr);
     OnDevice on(s->device);
     if (on.err != hipSuccess) return fail(s, SNN_EDEVICE, "hipSetDevice", hipGetErrorString(on.err));
     SampleArgs a{};

@@ -282,10 +282,12 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
     const float* Ap = a.A + (long long)c * a.state + 4 * q;
     const long long g0 = (long long)g * a.state + 4 * q;
     float y = 0.0f;
-    const bool whole = a.state % 4 == 0 && 4 * q < a.state;     // a 16-byte vector of its own
+    const bool whole = a.state % 4 == 0 && 4 * q < a.state;
+    typedef Vec<float, 4>::type F4;
     if (whole) {
-        const float4 A4 = *reinterpret_cast<const float4*>(Ap);
-        float4 h = a.h0 ? *reinterpret_cast<const float4*>(a.h0 + s0) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const F4 A4 = *reinterpret_cast<const F4*>(Ap);
+        F4 h = {};
+        if (a.h0) h = *reinterpret_cast<const F4*>(a.h0 + s0);
         h.x = fmaf(exp2_fast(d * (A4.x * kLog2e)), h.x, x * at(a.B, g0));
         h.y = fmaf(exp2_fast(d * (A4.y * kLog2e)), h.y, x * at(a.B, g0 + 1));
         h.z = fmaf(exp2_fast(d * (A4.z * kLog2e)), h.z, x * at(a.B, g0 + 2));
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
         y = fmaf(at(a.C, g0 + 1), h.y, y);
         y = fmaf(at(a.C, g0 + 2), h.z, y);
         y = fmaf(at(a.C, g0 + 3), h.w, y);
-        if (live) *reinterpret_cast<float4*>(a.hT + s0) = h;
+        if (live) *reinterpret_cast<F4*>(a.hT + s0) = h;
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)

@@ -681,3 +681,50 @@ def test_refusals():
                dict(recompute=True)):
         with pytest.raises(snn.SNNError):
             snn.SequenceLayer(**dict(dict(batch=B, T=T, channels=C), **kw))
+
+
+def test_outputs_that_are_inputs_and_sizes_past_a_launch_are_refused():
+    import paper_2501_07331_amd as snn
+    torch = _torch()
+    B, T, C = 2, 10, 6
+    L = _layer(B, T, C)
+    x = torch.zeros(B, T, C, device="cuda")
+    scale = torch.zeros(B, T, 1, device="cuda")
+    same = snn.Packed(x.view(-1).view(torch.uint8)[:B * T * C].view(B, T, C), scale)
+    onto = snn.Packed(torch.zeros(B, T, C, dtype=torch.uint8, device="cuda"), x.view(-1)[:B * T].view(B, T, 1))
+    i32 = x.view(-1).view(torch.int32)
+    ids = torch.zeros(60, dtype=torch.int32, device="cuda")
+    R = snn.Sampler(4, 5)
+    z, t = x.view(-1)[20:40].view(4, 5), torch.zeros(4, dtype=torch.int32, device="cuda")
+    u = x.view(-1)[:4]
+    bad = [lambda: L.pack(x, same), lambda: L.pack(x, onto), lambda: L.unpack(same, x), lambda: L.unpack(onto, x),
+           lambda: L.bin_spikes(i32[:B + 1], ids, ids, x), lambda: L.bin_records(ids[:B], i32[:B].view(B, 1), ids[:B].view(B, 1), x),
+           lambda: L.conv_forward(torch.ones_like(x), torch.zeros(C, 4, device="cuda"), None, x, lengths=i32[:B]),
+           lambda: R.sample(z, u, i32[:4]), lambda: R.sample(z, u, i32[20:24]), lambda: R.sample(z, u, t, logprob=u),
+           lambda: R.sample(z, u, t, top_k=t), lambda: R.sample(z, u, t, logprob=t.view(torch.float32)),
+           # batch x channels, batch x taps x channels, the sums of a training pass, rows
+           lambda: snn.SequenceLayer(65535, 1, 65536, state=8, taps=1), lambda: snn.SequenceLayer(65535, 1, 65536, state=4, taps=3),
+           lambda: snn.SequenceLayer(64, 65536, 64, state=64, groups=16, train=True), lambda: snn.Sampler(1 << 22, 4)]
+    for i, call in enumerate(bad):
+        print(f"[seq] refusal {i}", flush=True)
+        with pytest.raises(snn.SNNError) as e:
+            call()
+        assert "EINVAL" in str(e.value), (i, e.value)
+    R.sample(z, u, t)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("N", [4, 16])
+def test_a_step_with_states_at_odd_addresses(N):
+    torch = _torch()
+    B, C = 3, 10
+    L = _layer(B, 1, C, state=N)
+    f = lambda *s: torch.randn(*s, device="cuda")   # noqa: E731
+    torch.manual_seed(N)
+    x, d, bc, A, h = f(B, C), f(B, C), f(B, N), -f(C, N).abs(), f(B, C, N)
+    y, hT, y1 = f(B, C), f(B, C, N), f(B, C)
+    L.scan_step(x, d, A, bc, bc, h, hT, y)
+    off = [f(v.numel() + 1)[1:].view(v.shape) for v in (A, h, hT)]
+    off[0].copy_(A), off[1].copy_(h)
+    L.scan_step(x, d, off[0], bc, bc, off[1], off[2], y1)
+    assert torch.equal(y, y1) and torch.equal(hT, off[2])
