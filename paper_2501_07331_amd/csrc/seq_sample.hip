@@ -310,7 +310,7 @@ struct End {
     int last;
 };
 constexpr unsigned kOpen = ~0u;
-constexpr int kOpenMost = 1024;                    // most elements of an interval left open
+constexpr int kOpenMost = 8192;                    // most elements of an interval left open
 
 // The end in `inside` elements of one key: as many as the limits leave.
 __device__ __forceinline__ End end_in_key(const Row& r, unsigned key, unsigned inside, u64 inside_mass, u64 above,
@@ -360,12 +360,16 @@ __device__ __forceinline__ u64 lane_merge(u64 x, bool down) {
 
 // The end among the n <= NT elements of the list, which lies in w.mass and is
 // sorted there, one element a thread, by a bitonic network: exchanges within a
-// wave are between its lanes' registers.  w.n_kept of the elements are kept.
+// wave are between its lanes' registers.  w.n_kept of the elements are kept;
+// if none is, the end is before hi, which no element of the list is above.
 template <int NT>
-__device__ End end_in_list(const Row& r, unsigned n, u64 above, unsigned n_above, u64 limit, unsigned hi, Work<NT>& w) {
+__device__ End end_in_list(const Row& r, unsigned n, u64 above, unsigned n_above, u64 limit, u64 hi, Work<NT>& w) {
     static_assert(NT <= kBins, "the list takes the histogram's place");
     const unsigned tid = threadIdx.x, wave = tid / 64;
-    if (tid == 0) w.n_kept = 0, w.last_key = hi, w.last = (unsigned)-1, w.kept_mass = above;
+    if (tid == 0) {
+        w.n_kept = 0, w.last_key = list_key(hi), w.kept_mass = above;
+        w.last = ~(unsigned)hi > 0x7fffffffu ? 0x7fffffff : ~(unsigned)hi - 1;
+    }
     __syncthreads();
     u64 x = tid < n ? w.mass[tid] : 0;                 // 0 is below every element
     if (wave * 64 < n) {
@@ -465,7 +469,7 @@ __device__ End find_end(const SampleArgs& a, int row, const Row& r, unsigned top
                 const int at = atomicAdd(&w.listed, 1);
                 if (at < NT) w.mass[at] = in_list(key_of(z), i);     // always: they are the interval's `inside`
             });
-            return end_in_list(r, inside, above, n_above, limit, hi, w);
+            return end_in_list(r, inside, above, n_above, limit, in_list(hi, 0), w);
         }
         sh = 0;
         while ((hi - lo) >> sh >= (unsigned)kBins) ++sh;
@@ -817,7 +821,7 @@ __global__ void __launch_bounds__(kPartNT) sample_parts_kernel(SampleArgs a) {
 
 // The end in an open interval, if there is one; the part in which the running
 // sum passes the goal, and the index in it.
-constexpr int kDrawNT = kOpenMost;
+constexpr int kDrawNT = 1024;
 template <class T>
 __global__ void __launch_bounds__(kDrawNT) sample_draw_kernel(SampleArgs a) {
     __shared__ Work<kDrawNT> w;
@@ -830,10 +834,50 @@ __global__ void __launch_bounds__(kDrawNT) sample_draw_kernel(SampleArgs a) {
     End e{s.end_key, s.end_count, s.end_mass, 0x7fffffff};
     u64 goal = s.goal;
     if (s.open) {
+        const u64* list = open_list(a, row);
         const unsigned listed = min(s.listed, (unsigned)kOpenMost);
+        u64 above = s.above, lo = in_list(s.lo, 0x7fffffff), hi = in_list(s.hi, 0);
+        unsigned n_above = s.n_above, inside = listed;
+        // more than can be sorted: the part of the interval, by key and index, in which the end lies
+        // (4 rows of 250001, 0.3 wide, top-p 0.9, 5000 in the interval: 88 us, and 134 by whole rows in one workgroup)
+        while (inside > kDrawNT) {
+            int sh = 0;
+            while ((hi - lo) >> sh >= (u64)kBins) ++sh;
+            __syncthreads();
+            for (int i = tid; i < kBins; i += kDrawNT) w.mass[i] = 0, w.count[i] = 0;
+            __syncthreads();
+            for (unsigned i = tid; i < listed; i += kDrawNT) {
+                const u64 x = list[i];
+                if (x < lo || x > hi) continue;
+                bool kept;
+                const u64 v = r.weight(score_of(list_key(x)), kept);
+                const int bin = (int)((hi - x) >> sh);
+                if (v) atomicAdd(&w.mass[bin], v);
+                atomicAdd(&w.count[bin], 1u);
+            }
+            __syncthreads();
+            const int cb = find_cut(w, above, n_above, s.limit, (unsigned)r.top_k);
+            if (cb == kBins) break;                    // never: the limits are passed in it
+            above = w.above, n_above = w.n_above, inside = w.inside;
+            hi -= (u64)cb << sh;
+            if (hi - lo > (1ull << sh) - 1) lo = hi - ((1ull << sh) - 1);
+        }
+        if (tid == 0) w.listed = 0;
         for (int i = tid; i < a.parts; i += kDrawNT) more[i] = 0;
-        for (unsigned i = tid; i < listed; i += kDrawNT) w.mass[i] = open_list(a, row)[i];
-        e = end_in_list(r, listed, s.above, s.n_above, s.limit, s.hi, w);
+        if (listed <= kDrawNT && tid < listed) w.mass[tid] = list[tid];
+        __syncthreads();
+        for (unsigned i = tid; listed > kDrawNT && i < listed; i += kDrawNT) {
+            const u64 x = list[i];
+            if (x < lo) continue;
+            if (x <= hi) {
+                const int at = atomicAdd(&w.listed, 1);
+                if (at < kDrawNT) w.mass[at] = x;      // always: `inside` of them
+            } else {
+                bool kept;
+                atomicAdd(&more[list_index(x) / a.part_len], r.weight(score_of(list_key(x)), kept));
+            }
+        }
+        e = end_in_list(r, min(inside, (unsigned)kDrawNT), above, n_above, s.limit, hi, w);
         goal = share(e.mass, r.u, false);
         for (unsigned i = tid; i < w.n_kept; i += kDrawNT) {
             bool kept;

@@ -131,6 +131,19 @@ def test_few_equal_scores_far_apart(dtype):
     _run(z, u, dtype, top_k=np.full(R, few + 5), top_p=r.uniform(0.3, 1, R), min_p=np.where(np.arange(R) % 2, 0.98, 0.0))
 
 
+def test_many_scores_near_the_border():
+    """Thousands of scores within a hundredth of the one that the kept ones end at, all different or of a few values."""
+    r = np.random.default_rng(31)
+    R, V = 14, 130001
+    u = np.where(np.arange(R) % 3 == 0, 1 - 2.0 ** -24, r.random(R))
+    flat = (r.normal(size=(R, V)) * 0.3).astype(np.float32)
+    few = (r.integers(0, 200, size=(R, V)) * 0.003).astype(np.float32)
+    for z in (flat, few):
+        _run(z, u, "float32", top_p=np.linspace(0.01, 0.99, R))
+        _run(z, u, "float32", top_k=np.linspace(2, V - 1, R).astype(np.int64))
+        _run(z, u, "bfloat16", top_p=np.linspace(0.05, 0.95, R), top_k=np.full(R, V // 2), min_p=np.full(R, 0.3))
+
+
 def test_a_handle_serves_smaller_calls():
     """Rows and scores below the handle's: a row is divided otherwise for each call."""
     import torch
